@@ -1,0 +1,139 @@
+/*
+ * gemm_routed.h -- products whose rows choose their right operand, for MI355X (gfx950).
+ *
+ * Two things that models do beside plain products:
+ *   experts:   a router scores every expert for every token (gemm_route), the tokens' entries are sorted
+ *              by expert (gemm_route_plan), each expert multiplies its rows (gemm_grouped), and a token's
+ *              results are added up (gemm_combine); with the gradients of each step (gemm_route_backward,
+ *              gemm_grouped with the other layout, gemm_grouped_wgrad, gemm_combine_backward);
+ *   adapters:  the rows of one product carry low-rank additions of their own (gemm_adapters).
+ *
+ * Pointers, layouts, leading dimensions, streams, status codes and workspaces are those of gemm.h: every
+ * matrix and array is in DEVICE memory of the current device and stays the caller's; ld == 0 means packed;
+ * layouts are GEMM_ROW_MAJOR or GEMM_COL_MAJOR; matrices need element alignment only (multiples of 4 bytes of
+ * base, leading dimension and stride are faster, of 16 bytes fastest); int32 and float arrays 4 bytes; work is
+ * enqueued on hip_stream, nothing synchronises with the host, and a call that returns a negative status for its
+ * arguments has enqueued nothing.  Outputs must not overlap inputs.  All sums are held in binary32, and results do
+ * not depend on the order in which workgroups run.
+ *
+ * Device arrays of numbers (expert numbers, offsets, slots, adapter numbers) cannot be checked by the host.  The
+ * kernels check them: a number out of its range names nothing, as -1 does, and never makes a kernel read or write
+ * outside the arrays that the arguments describe.
+ */
+#ifndef MI355X_GEMM_ROUTED_H
+#define MI355X_GEMM_ROUTED_H
+
+#include "gemm.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* element types */
+enum { GEMM_ELEM_F32 = 0, GEMM_ELEM_F16 = 1, GEMM_ELEM_BF16 = 2 };
+
+/*
+ * Kinds: operand and result type, the GEMM_KIND_* of gemm.h and this one: bfloat16 operands, binary32 sums rounded
+ * once to bfloat16, to nearest even.
+ */
+enum { GEMM_KIND_BF16BF16 = 4 };
+
+/* scores of a router */
+enum { GEMM_SCORE_SOFTMAX = 0, GEMM_SCORE_SIGMOID = 1 };
+
+#define GEMM_ROUTE_MAX_EXPERTS 1024
+#define GEMM_ROUTE_MAX_GROUPS 64
+#define GEMM_ROUTE_MAX_TOP_K 64
+
+/*
+ * Routing.  logits: tokens x experts, row-major, element type `elem`.  Per token, in binary32:
+ *   s = softmax(logits) or sigmoid(logits);   c = s + bias   (bias: `experts` floats, or NULL; it decides who is
+ *   chosen and is no part of the weights);
+ *   groups > 1: the experts are `groups` equal consecutive groups; a group's score is the sum of its group_top (1 or 2)
+ *   highest c; only experts of the top_groups highest groups can be chosen;
+ *   the top_k experts of the highest c are chosen, in descending order;
+ *   weights = scale * s of these, divided by their sum if renormalise is not 0.
+ * Equal values go to the lowest index, of experts and of groups.  A logit of minus infinity masks an expert: its
+ * score is zero, and it is chosen only after all others; the scores of a row whose logits are all minus infinity
+ * are zero.  Where all scores that are to be renormalised are zero, the weights are zero.  A NaN ranks below every
+ * number; the weights it reaches are NaN, the chosen experts are distinct all the same.
+ * weights: tokens x top_k floats, indices: tokens x top_k int32, both packed.
+ * GEMM_ERR_INVALID_ARG: experts is not a multiple of groups, top_groups is not in 1 .. groups, group_top neither 1
+ * nor 2, or top_k more than the experts of top_groups groups.  GEMM_ERR_UNSUPPORTED beyond the limits above.
+ */
+int gemm_route(int elem, int64_t tokens, int64_t experts, const void *logits, int64_t ld, const float *bias, int score,
+               int64_t groups, int64_t top_groups, int group_top, int64_t top_k, int renormalise, float scale,
+               float *weights, int32_t *indices, void *hip_stream);
+
+/*
+ * Gradient of gemm_route's weights for the logits: d_logits (tokens x experts, element type `elem`, every element is
+ * written) from d_weights and the experts chosen (as gemm_route has written them: a token's are distinct).
+ */
+int gemm_route_backward(int elem, int64_t tokens, int64_t experts, const void *logits, int64_t ld, int score,
+                        int64_t top_k, int renormalise, float scale, const int32_t *indices, const float *d_weights,
+                        void *d_logits, int64_t ld_d, void *hip_stream);
+
+/*
+ * Sorts the entries (token, j) of indices (tokens x top_k) by expert, entries of one expert in the order of token
+ * and j: expert e has the slots offsets[e] .. offsets[e + 1] - 1.  offsets: experts + 1 int32; token_of[slot]:
+ * the slot's token, -1 behind the last slot (tokens * top_k int32); slot_of[token][j]: the entry's slot, -1 if
+ * its expert is not in 0 .. experts - 1.  At most GEMM_ROUTE_MAX_EXPERTS experts and less than 2^28 entries.
+ */
+int gemm_route_plan(int64_t tokens, int64_t top_k, int64_t experts, const int32_t *indices, int32_t *offsets,
+                    int32_t *token_of, int32_t *slot_of, void *hip_stream);
+
+/*
+ * C(i,:) = A(row(i),:) * B_e for the rows offsets[e] <= i < offsets[e + 1] of every group e, row(i) = row_map[i], or i
+ * if row_map is NULL.  A: a_rows x K, row-major; B_e = B + e * strideB elements, K x N, layoutB; C: rows x N, row-major.
+ * kind: GEMM_KIND_*.  offsets: groups + 1 int32 that do not decrease, of which what lies outside 0 .. rows is not
+ * used.  Rows of C in no group are not written; row(i) outside 0 .. a_rows - 1 is a row of zeros.  ld* == 0: packed,
+ * strideB == 0: matrices packed one after the other; a strideB below a matrix's extent lets the groups' matrices overlap.
+ * The gradient for A's rows is the same call on the gradient of C with the other layoutB and N, K exchanged.
+ */
+int gemm_grouped(int kind, int64_t groups, const int32_t *offsets, int64_t rows, int64_t N, int64_t K,
+                 const void *A, int64_t a_rows, int64_t lda, const int32_t *row_map,
+                 const void *B, int layoutB, int64_t ldb, int64_t strideB, void *C, int64_t ldc, void *hip_stream);
+
+/*
+ * C_e = sum over the group's rows i of A(row(i),:)^T * D(i,:), M x N, layoutC, C_e = C + e * strideC elements: the gradient of
+ * B_e from gemm_grouped's A (a_rows x M, row-major) and the gradient of its C (D: rows x N, row-major).  A group
+ * without rows gets zeros.  Rows as in gemm_grouped.  strideC == 0: packed; otherwise at least a matrix's extent.
+ */
+int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t rows, int64_t M, int64_t N,
+                       const void *A, int64_t a_rows, int64_t lda, const int32_t *row_map,
+                       const void *D, int64_t ldd, void *C, int layoutC, int64_t ldc, int64_t strideC, void *hip_stream);
+
+/*
+ * out(t,:) = sum over j of weights[t][j] * Y(slot_of[t][j],:), j ascending; weights NULL: ones.  Y: y_rows x N, out: tokens x N,
+ * row-major, kind: their types.  A slot outside 0 .. y_rows - 1 adds nothing (whatever its weight).
+ */
+int gemm_combine(int kind, int64_t tokens, int64_t top_k, int64_t N, const void *Y, int64_t y_rows, int64_t ldy,
+                 const int32_t *slot_of, const float *weights, void *out, int64_t ldo, void *hip_stream);
+
+/*
+ * Its gradients: dY(slot_of[t][j],:) = weights[t][j] * d_out(t,:) (rows of dY that are no entry's slot are not
+ * written; slots are distinct) and d_weights[t][j] = <d_out(t,:), Y(slot_of[t][j],:)> (zero where there is no such slot).
+ * elem: the type of d_out, Y and dY.  weights NULL: ones; d_weights NULL: left out, and Y is not read.
+ */
+int gemm_combine_backward(int elem, int64_t tokens, int64_t top_k, int64_t N, const void *d_out, int64_t ldo,
+                          const void *Y, int64_t y_rows, int64_t ldy, const int32_t *slot_of, const float *weights,
+                          void *dY, int64_t lddy, float *d_weights, void *hip_stream);
+
+/*
+ * C(i,:) = A(i,:) * B + scales[a] * (A(i,:) * down_a) * up_a with a = adapter_of[i]; rows whose a is outside 0 .. adapters - 1 have
+ * no addition.  A: rows x K, C: rows x N, row-major; B: K x N, layoutB; down_a = down + a * stride_down elements, K x rank,
+ * layout_down; up_a: rank x N, likewise; scales NULL: ones.  Rows of one adapter need not be neighbours, but a run of
+ * them shares what is read.  The sum is rounded once; A(i,:) * down_a is held to 22 bits or more.  rank is at most 256.
+ * The gradient for A is the same call on the gradient of C with N and K exchanged, the other layoutB, and down and up
+ * exchanged, each with its other layout.
+ */
+#define GEMM_ADAPTERS_MAX_RANK 256
+int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, int64_t lda, const void *B, int layoutB, int64_t ldb,
+                  int64_t adapters, int64_t rank, const int32_t *adapter_of, const float *scales,
+                  const void *down, int layout_down, int64_t ld_down, int64_t stride_down,
+                  const void *up, int layout_up, int64_t ld_up, int64_t stride_up, void *C, int64_t ldc, void *hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MI355X_GEMM_ROUTED_H */

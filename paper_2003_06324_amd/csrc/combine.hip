@@ -1,0 +1,197 @@
+// The weighted sum of a token's rows and its gradients.
+#include "routed_common.h"
+
+using namespace gemm_gfx950;
+
+namespace {
+
+constexpr int COMBINE_THREADS = 256;
+
+// EL neighbouring elements, 16 bytes of 16-bit types and of binary32; element alignment is enough
+template <typename T> struct Piece {
+    static constexpr int EL = 16 / (int)sizeof(T);
+    typedef T vec_t __attribute__((ext_vector_type(EL)));
+    typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+
+    static __device__ __forceinline__ void load(const T *p, int valid, float (&out)[EL])
+    {
+        if (valid >= EL) {
+            const vec_t v = *(const loose_t *)p;
+#pragma unroll
+            for (int x = 0; x < EL; ++x) out[x] = (float)v[x];
+        } else {
+#pragma unroll
+            for (int x = 0; x < EL; ++x) out[x] = x < valid ? (float)p[x] : 0.0f;
+        }
+    }
+    static __device__ __forceinline__ void store(T *p, int valid, const float *v)
+    {
+        if (valid >= EL) {
+            vec_t o;
+#pragma unroll
+            for (int x = 0; x < EL; ++x) o[x] = rounded<T>(v[x]);
+            *(loose_t *)p = o;
+            behind_wide_store();
+        } else {
+#pragma unroll
+            for (int x = 0; x < EL; ++x)
+                if (x < valid) p[x] = rounded<T>(v[x]);
+        }
+    }
+};
+
+struct CombineArgs {
+    const void *Y;
+    const int32_t *slot_of;
+    const float *weights;
+    void *out;
+    int64_t tokens, ldy, ldo;
+    int y_rows, top_k, N, per_row;  // per_row: threads of a token, a power of two
+};
+
+// ---------------------------------------------------------------------------
+// A thread adds up one piece of 16 bytes of a token's rows, eight of them asked for at once.  Nothing but the rows is moved.
+// ---------------------------------------------------------------------------
+template <typename T, typename TC> __global__ __launch_bounds__(COMBINE_THREADS) void combine_kernel(const CombineArgs p)
+{
+    constexpr int EL = Piece<T>::EL, AHEAD = 8;
+    const int64_t t = (int64_t)blockIdx.x * (COMBINE_THREADS / p.per_row) + threadIdx.x / p.per_row;
+    const int64_t col = ((int64_t)blockIdx.y * p.per_row + threadIdx.x % p.per_row) * EL;
+    if (t >= p.tokens || col >= p.N) return;
+    const int valid = p.N - (int)col < EL ? p.N - (int)col : EL;
+    float acc[EL];
+#pragma unroll
+    for (int x = 0; x < EL; ++x) acc[x] = 0.0f;
+    for (int j0 = 0; j0 < p.top_k; j0 += AHEAD) {
+        float w[AHEAD], y[AHEAD][EL];
+        bool there[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int slot = j0 + j < p.top_k ? p.slot_of[t * p.top_k + j0 + j] : -1;
+            there[j] = slot >= 0 && slot < p.y_rows;
+            w[j] = there[j] && p.weights != nullptr ? p.weights[t * p.top_k + j0 + j] : 1.0f;
+            if (there[j]) Piece<T>::load((const T *)p.Y + slot * p.ldy + col, valid, y[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (there[j]) {
+#pragma unroll
+                for (int x = 0; x < EL; ++x) acc[x] = fmaf(w[j], y[j][x], acc[x]);
+            }
+    }
+    TC *o = (TC *)p.out + t * p.ldo + col;
+    if constexpr (sizeof(TC) == sizeof(T)) {
+        Piece<TC>::store(o, valid, acc);
+    } else {  // binary32 from 16-bit rows: two pieces
+        Piece<TC>::store(o, valid, acc);
+        if (valid > EL / 2) Piece<TC>::store(o + EL / 2, valid - EL / 2, acc + EL / 2);
+    }
+}
+
+struct CombineBackwardArgs {
+    const void *d_out, *Y;
+    const int32_t *slot_of;
+    const float *weights;
+    void *dY;
+    float *d_weights;
+    int64_t entries, ldo, ldy, lddy;
+    int y_rows, N;
+    Divisor by_k;
+};
+
+// ---------------------------------------------------------------------------
+// A wave an entry: it reads the token's d_out (which its neighbours read too, so memory is asked for it once) and the entry's row, and writes
+// the entry's row of dY.  The scalar product is added up piece by piece, then over the lanes, always in the same order.
+// ---------------------------------------------------------------------------
+template <typename T> __global__ __launch_bounds__(COMBINE_THREADS) void combine_backward_kernel(const CombineBackwardArgs p)
+{
+    constexpr int EL = Piece<T>::EL;
+    const int64_t n = (int64_t)blockIdx.x * (COMBINE_THREADS / 64) + threadIdx.x / 64;
+    const int lane = threadIdx.x & 63;
+    if (n >= p.entries) return;
+    const int slot = p.slot_of[n];
+    if (slot < 0 || slot >= p.y_rows) {
+        if (p.d_weights != nullptr && lane == 0) p.d_weights[n] = 0.0f;
+        return;
+    }
+    const float w = p.weights != nullptr ? p.weights[n] : 1.0f;
+    const T *d = (const T *)p.d_out + (int64_t)divide((int)n, p.by_k) * p.ldo;
+    const T *y = (const T *)p.Y + slot * p.ldy;
+    T *dy = (T *)p.dY + slot * p.lddy;
+    float dot = 0.0f;
+#pragma unroll 4
+    for (int64_t col = lane * EL; col < p.N; col += 64 * EL) {
+        const int valid = p.N - col < EL ? (int)(p.N - col) : EL;
+        float dv[EL], out[EL];
+        Piece<T>::load(d + col, valid, dv);
+        if (p.d_weights != nullptr) {
+            float yv[EL];
+            Piece<T>::load(y + col, valid, yv);
+#pragma unroll
+            for (int x = 0; x < EL; ++x) dot = x < valid ? fmaf(dv[x], yv[x], dot) : dot;
+        }
+#pragma unroll
+        for (int x = 0; x < EL; ++x) out[x] = w * dv[x];
+        Piece<T>::store(dy + col, valid, out);
+    }
+    if (p.d_weights == nullptr) return;
+    for (int s = 1; s < 64; s <<= 1) dot += __shfl_xor(dot, s);
+    if (lane == 0) p.d_weights[n] = dot;
+}
+
+template <typename T, typename TC> int launch_combine(const CombineArgs &a, hipStream_t s)
+{
+    const int64_t pieces = ceil_div(a.N, Piece<T>::EL);
+    CombineArgs b = a;
+    b.per_row = 1;
+    while (b.per_row < COMBINE_THREADS && b.per_row < pieces) b.per_row *= 2;
+    const dim3 grid((unsigned)ceil_div(a.tokens, COMBINE_THREADS / b.per_row), (unsigned)ceil_div(pieces, b.per_row));
+    return enqueue(combine_kernel<T, TC>, grid, dim3(COMBINE_THREADS), s, b);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gemm_combine(int kind, int64_t tokens, int64_t top_k, int64_t N, const void *Y, int64_t y_rows, int64_t ldy,
+                 const int32_t *slot_of, const float *weights, void *out, int64_t ldo, void *hip_stream)
+{
+    if (!valid_kind(kind) || tokens < 0 || top_k < 0 || N < 0 || y_rows < 0 || ldy < 0 || ldo < 0) return GEMM_ERR_INVALID_ARG;
+    if (!fill_ld(GEMM_ROW_MAJOR, ldy, y_rows, N) || !fill_ld(GEMM_ROW_MAJOR, ldo, tokens, N)) return GEMM_ERR_INVALID_ARG;
+    if (tokens > kMaxExtent || N > kMaxExtent || y_rows > kMaxExtent || top_k > kMaxExtent || too_far(y_rows, ldy) || too_far(tokens, ldo) ||
+        too_far(tokens, top_k))
+        return GEMM_ERR_UNSUPPORTED;
+    if (tokens == 0 || N == 0) return GEMM_OK;
+    if (out == nullptr || (top_k > 0 && slot_of == nullptr) || (y_rows > 0 && top_k > 0 && Y == nullptr)) return GEMM_ERR_INVALID_ARG;
+    const CombineArgs a = {Y, slot_of, weights, out, tokens, ldy, ldo, (int)y_rows, (int)top_k, (int)N, 0};
+    const hipStream_t s = (hipStream_t)hip_stream;
+    switch (kind) {
+    case GEMM_KIND_F32: return launch_combine<float, float>(a, s);
+    case GEMM_KIND_F16F32: return launch_combine<_Float16, float>(a, s);
+    case GEMM_KIND_F16F16: return launch_combine<_Float16, _Float16>(a, s);
+    case GEMM_KIND_BF16F32: return launch_combine<__bf16, float>(a, s);
+    default: return launch_combine<__bf16, __bf16>(a, s);
+    }
+}
+
+int gemm_combine_backward(int elem, int64_t tokens, int64_t top_k, int64_t N, const void *d_out, int64_t ldo,
+                          const void *Y, int64_t y_rows, int64_t ldy, const int32_t *slot_of, const float *weights,
+                          void *dY, int64_t lddy, float *d_weights, void *hip_stream)
+{
+    if (!valid_elem(elem) || tokens < 0 || top_k < 0 || N < 0 || y_rows < 0 || ldy < 0 || ldo < 0 || lddy < 0) return GEMM_ERR_INVALID_ARG;
+    if (!fill_ld(GEMM_ROW_MAJOR, ldy, y_rows, N) || !fill_ld(GEMM_ROW_MAJOR, lddy, y_rows, N) || !fill_ld(GEMM_ROW_MAJOR, ldo, tokens, N))
+        return GEMM_ERR_INVALID_ARG;
+    if (N > kMaxExtent || y_rows > kMaxExtent || too_far(y_rows, ldy) || too_far(y_rows, lddy) || too_far(tokens, ldo) ||
+        tokens > (1LL << 28) - 1 || top_k > (1LL << 28) - 1 || tokens * top_k > (1LL << 28) - 1)
+        return GEMM_ERR_UNSUPPORTED;
+    if (tokens == 0 || top_k == 0) return GEMM_OK;
+    if (slot_of == nullptr || (N > 0 && (d_out == nullptr || (y_rows > 0 && (dY == nullptr || (d_weights != nullptr && Y == nullptr))))))
+        return GEMM_ERR_INVALID_ARG;
+    const CombineBackwardArgs a = {d_out, Y, slot_of, weights, dY, d_weights, tokens * top_k, ldo, ldy, lddy, (int)y_rows, (int)N, divisor(top_k)};
+    const dim3 grid((unsigned)ceil_div(a.entries, COMBINE_THREADS / 64)), block(COMBINE_THREADS);
+    const hipStream_t s = (hipStream_t)hip_stream;
+    if (elem == GEMM_ELEM_F32) return enqueue(combine_backward_kernel<float>, grid, block, s, a);
+    return elem == GEMM_ELEM_F16 ? enqueue(combine_backward_kernel<_Float16>, grid, block, s, a) : enqueue(combine_backward_kernel<__bf16>, grid, block, s, a);
+}
+
+}  // extern "C"

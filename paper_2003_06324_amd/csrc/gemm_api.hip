@@ -3,6 +3,7 @@
 // kernel launches on the caller's stream.  No host synchronisation.
 #include "gemm.h"
 #include "gemm_launch.h"
+#include "routed_common.h"
 
 #include <algorithm>
 #include <cmath>
@@ -711,6 +712,26 @@ int static_scratch(DeviceState &d, void **out)
     *out = d.static_scratch;
     return GEMM_OK;
 }
+
+}  // namespace
+
+// (for the entry points of gemm_routed.h; under capture a workspace is used as it is or not at all)
+int gemm_gfx950::stream_scratch(hipStream_t stream, size_t bytes, StreamScratch &out)
+{
+    out.lock = std::unique_lock<std::mutex>(g_mutex);
+    DeviceState *dev = nullptr;
+    if (device_state(&dev) != GEMM_OK) return GEMM_ERR_HIP;
+    out.num_cu = dev->num_cu;
+    if (bytes == 0) return GEMM_OK;
+    if (stream_workspace(*dev, stream).bytes < bytes) {
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        if (hipStreamIsCapturing(stream, &status) != hipSuccess) (void)hipGetLastError();
+        else if (status == hipStreamCaptureStatusActive) return GEMM_ERR_WORKSPACE;
+    }
+    return get_workspace(*dev, stream, bytes, &out.ptr);
+}
+
+namespace {
 
 // T: operand type (bfloat16 runs the binary16 path with the other MFMA instruction, so it shares
 // the binary16 slab times of the selection); TC: element type of C (float, or _Float16 for gemm_f16f16).

@@ -1,0 +1,571 @@
+// Routing to experts: scores, choice and weights, their gradient, and the plan (entries sorted by expert).
+#include "routed_common.h"
+
+using namespace gemm_gfx950;
+
+namespace {
+
+constexpr int ROUTE_THREADS = 256;
+
+// Order of choice values as whole numbers: NaN 1, minus infinity next, the numbers ascending (both zeros alike).  0: not to be chosen.
+__device__ __forceinline__ uint32_t order_of(float c)
+{
+    const uint32_t u = __float_as_uint(c + 0.0f);
+    const uint32_t k = (u >> 31) != 0 ? ~u : u | 0x80000000u;
+    return c != c ? 1u : k;
+}
+
+template <typename T> __device__ __forceinline__ float as_float(T v) { return (float)v; }
+
+// The V logits of a lane (experts V * lane ..), minus infinity behind the last expert.  WIDE: rows and lanes begin on the boundaries
+// of what a lane reads at once and E is a multiple of V.
+template <typename T, int V, bool WIDE> __device__ __forceinline__ void load_logits(const T *row, int e0, int E, float (&l)[V])
+{
+    if constexpr (WIDE) {
+        constexpr int BYTES = V * (int)sizeof(T);
+        constexpr int PIECE = BYTES < 16 ? BYTES : 16, EL = PIECE / (int)sizeof(T);
+        struct alignas(PIECE) piece_t { T v[EL]; };
+#pragma unroll
+        for (int i = 0; i < V / EL; ++i) {
+            piece_t p;
+            if (e0 < E) p = *(const piece_t *)(row + e0 + i * EL);
+#pragma unroll
+            for (int x = 0; x < EL; ++x) l[i * EL + x] = e0 < E ? as_float(p.v[x]) : -INFINITY;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] = e0 + v < E ? as_float(row[e0 + v]) : -INFINITY;
+    }
+}
+
+// Scores of a lane's experts, in place.  Softmax: of a row of nothing but minus infinity zeros; a NaN or plus infinity makes all NaN.
+template <int L, int V> __device__ __forceinline__ void scores(float (&s)[V], bool softmax)
+{
+    if (softmax) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < V; ++v) m = fmaxf(m, s[v]);   // (passes NaN over; the sum below finds it)
+        m = max_over<L>(m);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float z = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            s[v] = expf(s[v] - base);
+            z += s[v];
+        }
+        z = sum_over<L>(z);
+        const float d = z > 0.0f ? 1.0f / z : (z == 0.0f ? 0.0f : z);
+#pragma unroll
+        for (int v = 0; v < V; ++v) s[v] = s[v] * d;
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) s[v] = 1.0f / (1.0f + expf(-s[v]));
+    }
+}
+
+struct RouteArgs {
+    const void *logits;
+    const float *bias;
+    float *weights;
+    int32_t *indices;
+    int64_t tokens, ld;
+    int E, groups, top_groups, group_top, group_size, top_k, softmax, renormalise;
+    float scale;
+    Divisor by_group;      // group_size
+    int lanes_per_group;   // where a group is this many whole lanes, a power of two; else 0
+};
+
+// ---------------------------------------------------------------------------
+// L lanes a token, V neighbouring experts a lane.  Scores and choice values stay in registers; a round of the choice is a maximum
+// over the lane's values, one over the lanes, and the lowest index of those that equal it.
+// Bound: reading the logits is little (16384 x 256 in bfloat16: 8 MB, 1.5 us); the instructions of top_k rounds are what it takes,
+// so a token gets as few lanes as its experts fit into the registers of (a wave then works on four at once), and the
+// lanes meet by data-parallel moves instead of shared memory.
+// ---------------------------------------------------------------------------
+template <typename T, int L, int V, bool WIDE>
+__global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
+{
+    const int64_t t = ((int64_t)blockIdx.x * ROUTE_THREADS + threadIdx.x) / L;
+    const int lane = threadIdx.x % L;
+    const bool live = t < p.tokens;   // (a wave's lanes stay together for the moves between them)
+    const int e0 = lane * V;
+    float s[V];
+    load_logits<T, V, WIDE>((const T *)p.logits + (live ? t : p.tokens - 1) * p.ld, e0, p.E, s);
+    scores<L, V>(s, p.softmax != 0);
+    uint32_t key[V];
+    float c[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        c[v] = p.bias != nullptr && e0 + v < p.E ? s[v] + p.bias[e0 + v] : s[v];
+        key[v] = e0 + v < p.E ? order_of(c[v]) : 0u;
+    }
+    if (p.groups > 1) {
+        // a group's score, in the end in the lane of the group's number
+        uint32_t rank = 0;
+        auto two = [&](uint32_t k1, uint32_t k2, float c1, float c2) {
+            // sum of the two highest (one where the group has but one, or one is asked for); NaN if either is
+            return p.group_top == 2 && k2 != 0 ? order_of(c1 + c2) : k1;
+        };
+        // the two highest of a and b, the pairs' order known
+        struct Two { uint32_t k1, k2; float c1, c2; };
+        auto add = [](Two &a, uint32_t k, float v) {
+            const bool first = k > a.k1, second = k > a.k2;
+            a.k2 = first ? a.k1 : (second ? k : a.k2);
+            a.c2 = first ? a.c1 : (second ? v : a.c2);
+            a.k1 = first ? k : a.k1;
+            a.c1 = first ? v : a.c1;
+        };
+        auto meet = [&](Two &a, auto step) {
+            constexpr int S = decltype(step)::value;
+            const uint32_t k1 = partner<S>(a.k1), k2 = partner<S>(a.k2);
+            const float c1 = __uint_as_float(partner<S>(__float_as_uint(a.c1))), c2 = __uint_as_float(partner<S>(__float_as_uint(a.c2)));
+            add(a, k1, c1);
+            add(a, k2, c2);
+        };
+        typedef std::integral_constant<int, 0> S0;
+        typedef std::integral_constant<int, 1> S1;
+        typedef std::integral_constant<int, 2> S2;
+        typedef std::integral_constant<int, 3> S3;
+        typedef std::integral_constant<int, 4> S4;
+        typedef std::integral_constant<int, 5> S5;
+        if (p.lanes_per_group > 0) {
+            Two m = {0, 0, 0.0f, 0.0f};
+#pragma unroll
+            for (int v = 0; v < V; ++v) add(m, key[v], c[v]);
+            const int n = p.lanes_per_group;
+            if (n > 1) meet(m, S0());
+            if (n > 2) meet(m, S1());
+            if (n > 4) meet(m, S2());
+            if (n > 8) meet(m, S3());
+            if constexpr (L == 64) {
+                if (n > 16) meet(m, S4());
+                if (n > 32) meet(m, S5());
+            }
+            const uint32_t mine = two(m.k1, m.k2, m.c1, m.c2);
+            rank = (uint32_t)__shfl((int)mine, lane * n < L ? lane * n : 0, L);
+        } else {
+            for (int g = 0; g < p.groups; ++g) {
+                Two m = {0, 0, 0.0f, 0.0f};
+#pragma unroll
+                for (int v = 0; v < V; ++v) add(m, divide(e0 + v, p.by_group) == g ? key[v] : 0u, c[v]);
+                meet(m, S0());
+                meet(m, S1());
+                meet(m, S2());
+                meet(m, S3());
+                if constexpr (L == 64) {
+                    meet(m, S4());
+                    meet(m, S5());
+                }
+                if (lane == g) rank = two(m.k1, m.k2, m.c1, m.c2);
+            }
+        }
+        int better = 0;
+        for (int g = 0; g < p.groups; ++g) {
+            const uint32_t other = (uint32_t)__shfl((int)rank, g, L);
+            better += other > rank || (other == rank && g < lane) ? 1 : 0;
+        }
+        const uint64_t kept = __ballot(lane < p.groups && better < p.top_groups) >> ((threadIdx.x & 63) / L * L);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int g = p.lanes_per_group > 0 ? lane / p.lanes_per_group : divide(e0 + v, p.by_group);
+            if (((kept >> (g & 63)) & 1) == 0) key[v] = 0;
+        }
+    }
+    // round j: the winner's index and score end up in lane j
+    int my_index = 0;
+    float my_score = 0.0f;
+    for (int j = 0; j < p.top_k; ++j) {
+        uint32_t m = key[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) m = key[v] > m ? key[v] : m;
+        m = umax_over<L>(m);
+        uint32_t at = 0xffffffffu;
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v) at = key[v] == m ? (uint32_t)(e0 + v) : at;
+        at = umin_over<L>(at);
+        float w = 0.0f;
+        uint32_t taken = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const bool it = at == (uint32_t)(e0 + v);
+            taken = it ? __float_as_uint(s[v]) : taken;
+            key[v] = it ? 0u : key[v];
+        }
+        w = __uint_as_float(over_lanes<L>(taken, [](uint32_t a, uint32_t b) { return a | b; }));
+        if (lane == j) {
+            my_index = (int)at;
+            my_score = w;
+        }
+    }
+    float out = my_score * p.scale;
+    if (p.renormalise) {
+        const float z = sum_over<L>(my_score);   // (lanes from top_k on hold zeros)
+        out = z == 0.0f ? 0.0f : my_score / z * p.scale;
+    }
+    if (live && lane < p.top_k) {
+        p.weights[t * p.top_k + lane] = out;
+        p.indices[t * p.top_k + lane] = my_index;
+    }
+}
+
+struct RouteBackwardArgs {
+    const void *logits;
+    const int32_t *indices;
+    const float *d_weights;
+    void *d_logits;
+    int64_t tokens, ld, ld_d;
+    int E, top_k, softmax, renormalise;
+    float scale;
+};
+
+// ---------------------------------------------------------------------------
+// With scores s, the chosen set S, Z = sum of s over S:  d_s = scale * dw, renormalised scale / Z * (dw - sum(dw s) / Z); then
+//   softmax: d_l = s (d_s - sum over S of d_s s);   sigmoid: d_l = d_s s (1 - s) on S, else zero.
+// Lane j deals with the token's chosen expert j, whose gradient goes to its expert's lane through shared memory.  Renormalised
+// softmax weights do not depend on the logits outside S: the sum over S of d_s s is zero there, and is left out.
+// ---------------------------------------------------------------------------
+template <typename T, int L, int V, bool WIDE>
+__global__ __launch_bounds__(ROUTE_THREADS) void route_backward_kernel(const RouteBackwardArgs p)
+{
+    __shared__ float grad[ROUTE_THREADS / L][L * V];
+    const int64_t t = ((int64_t)blockIdx.x * ROUTE_THREADS + threadIdx.x) / L;
+    const int lane = threadIdx.x % L, mine = threadIdx.x / L;
+    const bool live = t < p.tokens;
+    const int64_t row = live ? t : p.tokens - 1;
+    const int e0 = lane * V;
+    float s[V];
+    load_logits<T, V, WIDE>((const T *)p.logits + row * p.ld, e0, p.E, s);
+    scores<L, V>(s, p.softmax != 0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) grad[mine][e0 + v] = s[v];
+    __syncthreads();
+    int at = -1;
+    float dw = 0.0f, sj = 0.0f;
+    if (lane < p.top_k) {
+        at = p.indices[row * p.top_k + lane];
+        dw = p.d_weights[row * p.top_k + lane];
+        if (at < 0 || at >= p.E) at = -1;
+        if (at >= 0) sj = grad[mine][at];
+        else dw = 0.0f;
+    }
+    float ds;
+    if (p.renormalise) {
+        const float z = sum_over<L>(sj);
+        const float mean = z == 0.0f ? 0.0f : sum_over<L>(at >= 0 ? dw * (sj / z) : 0.0f);
+        ds = z == 0.0f ? 0.0f : p.scale * (dw - mean) / z;
+    } else {
+        ds = p.scale * dw;
+    }
+    if (at < 0) ds = 0.0f;
+    const float all = p.softmax && !p.renormalise ? sum_over<L>(ds * sj) : 0.0f;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) grad[mine][e0 + v] = 0.0f;
+    __syncthreads();
+    if (at >= 0) grad[mine][at] = ds;
+    __syncthreads();
+    if (!live) return;
+    T out[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const float g = grad[mine][e0 + v];
+        out[v] = rounded<T>(p.softmax ? s[v] * (g - all) : g * s[v] * (1.0f - s[v]));
+    }
+    T *d = (T *)p.d_logits + t * p.ld_d;
+    if constexpr (WIDE) {
+        constexpr int BYTES = V * (int)sizeof(T);
+        constexpr int PIECE = BYTES < 16 ? BYTES : 16, EL = PIECE / (int)sizeof(T);
+        struct alignas(PIECE) piece_t { T v[EL]; };
+        if (e0 < p.E) {
+#pragma unroll
+            for (int i = 0; i < V / EL; ++i) {
+                piece_t piece;
+#pragma unroll
+                for (int x = 0; x < EL; ++x) piece.v[x] = out[i * EL + x];
+                *(piece_t *)(d + e0 + i * EL) = piece;
+                behind_wide_store();
+            }
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (e0 + v < p.E) d[e0 + v] = out[v];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The plan: a stable counting sort.  A workgroup takes PLAN_WAVES * steps * 64 consecutive entries, a wave steps * 64 of them; within
+// a step of 64 entries an entry's place among those of its expert is the number of lower lanes with the same expert.
+// One workgroup does all of it where the entries are few; otherwise a first launch writes each workgroup's counts
+// and a second one adds up those of the workgroups before its own.
+// ---------------------------------------------------------------------------
+constexpr int64_t kMaxEntries = (1LL << 28) - 1;  // what Divisor divides
+constexpr int PLAN_WAVES = 16, PLAN_THREADS = PLAN_WAVES * 64;
+
+struct PlanArgs {
+    const int32_t *indices;
+    int32_t *offsets, *token_of, *slot_of, *counts;  // counts: [workgroup][E]
+    int64_t entries;
+    int E, steps, bits;  // bits: of an expert's number
+    Divisor by_k;        // top_k
+};
+
+// lanes of the wave whose entry has the same expert
+__device__ __forceinline__ uint64_t same_expert(int e, bool valid, int bits)
+{
+    uint64_t m = __ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((e >> b) & 1);
+        m &= (e >> b) & 1 ? set : ~set;
+    }
+    return m;
+}
+
+// this wave's counts to hist (its own E words, zeroed before)
+__device__ __forceinline__ void count_entries(const PlanArgs &p, int64_t first, int lane, int *hist)
+{
+    for (int i = 0; i < p.steps; ++i) {
+        const int64_t n = first + i * 64 + lane;
+        const int e = n < p.entries ? p.indices[n] : -1;
+        if (e >= 0 && e < p.E) atomicAdd(&hist[e], 1);  // (whole numbers: the order does not matter)
+    }
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void plan_count_kernel(const PlanArgs p)
+{
+    extern __shared__ int hist[];  // [E]
+    for (int e = threadIdx.x; e < p.E; e += PLAN_THREADS) hist[e] = 0;
+    __syncthreads();
+    count_entries(p, ((int64_t)blockIdx.x * PLAN_WAVES + threadIdx.x / 64) * p.steps * 64, threadIdx.x & 63, hist);
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.E; e += PLAN_THREADS) p.counts[(int64_t)blockIdx.x * p.E + e] = hist[e];
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void plan_place_kernel(const PlanArgs p)
+{
+    extern __shared__ int hist[];  // [PLAN_WAVES][E] a wave's next slot per expert, then [PLAN_WAVES] sums
+    int *const sums = hist + PLAN_WAVES * p.E;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    for (int i = tid; i < PLAN_WAVES * p.E; i += PLAN_THREADS) hist[i] = 0;
+    __syncthreads();
+    const int64_t first = ((int64_t)blockIdx.x * PLAN_WAVES + wave) * p.steps * 64;
+    count_entries(p, first, lane, hist + wave * p.E);
+    __syncthreads();
+    // thread e: entries of expert e before this workgroup, and in all of them
+    int before = 0, total = 0;
+    if (tid < p.E) {
+        if (gridDim.x == 1) {
+            for (int w = 0; w < PLAN_WAVES; ++w) total += hist[w * p.E + tid];
+        } else {
+            for (int b = 0; b < (int)gridDim.x; ++b) {
+                const int c = p.counts[(int64_t)b * p.E + tid];
+                before += b < (int)blockIdx.x ? c : 0;
+                total += c;
+            }
+        }
+    }
+    // sum of the totals of lower experts
+    int upto = total;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(upto, d);
+        if (lane >= d) upto += x;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int base = upto - total;
+    for (int w = 0; w < wave; ++w) base += sums[w];
+    int all = 0;
+    for (int w = 0; w < PLAN_WAVES; ++w) all += sums[w];
+    if (tid < p.E) {
+        if (blockIdx.x == 0) p.offsets[tid] = base;
+        int next = base + before;
+        for (int w = 0; w < PLAN_WAVES; ++w) {
+            const int c = hist[w * p.E + tid];
+            hist[w * p.E + tid] = next;
+            next += c;
+        }
+    }
+    if (blockIdx.x == 0 && tid == 0) p.offsets[p.E] = all;
+    __syncthreads();
+    int *const next = hist + wave * p.E;
+    for (int i = 0; i < p.steps; ++i) {
+        const int64_t n = first + i * 64 + lane;
+        const bool inside = n < p.entries;
+        const int e = inside ? p.indices[n] : -1;
+        const bool valid = e >= 0 && e < p.E;
+        const uint64_t same = same_expert(e, valid, p.bits);
+        const int lower = __popcll(same & ((1ull << lane) - 1));
+        int slot = -1;
+        if (valid) slot = next[e] + lower;
+        asm volatile("" ::: "memory");  // all lanes have read it (a wave's shared-memory operations are in order)
+        if (valid && lower == 0) next[e] = slot + __popcll(same);
+        asm volatile("" ::: "memory");
+        if (inside) p.slot_of[n] = slot;
+        if (valid) p.token_of[slot] = divide((int)n, p.by_k);
+        // behind the last slot: as many entries as name no expert, dealt out to the threads
+        if (inside && n >= all) p.token_of[n] = -1;
+    }
+}
+
+template <typename T, int L, int V> int launch_route(const RouteArgs &a, bool wide, hipStream_t s)
+{
+    const dim3 grid((unsigned)ceil_div(a.tokens, ROUTE_THREADS / L));
+    return wide ? enqueue(route_kernel<T, L, V, true>, grid, dim3(ROUTE_THREADS), s, a)
+                : enqueue(route_kernel<T, L, V, false>, grid, dim3(ROUTE_THREADS), s, a);
+}
+template <typename T, int L, int V> int launch_backward(const RouteBackwardArgs &a, bool wide, hipStream_t s)
+{
+    const dim3 grid((unsigned)ceil_div(a.tokens, ROUTE_THREADS / L));
+    return wide ? enqueue(route_backward_kernel<T, L, V, true>, grid, dim3(ROUTE_THREADS), s, a)
+                : enqueue(route_backward_kernel<T, L, V, false>, grid, dim3(ROUTE_THREADS), s, a);
+}
+
+// lanes a token and experts a lane: sixteen lanes where experts, groups and rounds fit them
+struct RouteShape { int L, V; };
+RouteShape route_shape(int64_t E, int64_t groups, int64_t top_k)
+{
+    RouteShape r;
+    r.L = E <= 256 && groups <= 16 && top_k <= 16 ? 16 : 64;
+    r.V = 1;
+    while (r.L * r.V < E) r.V *= 2;
+    return r;
+}
+// whether lanes may read (and write) their experts in pieces of up to 16 bytes
+bool lanes_wide(const void *p, int64_t ld, int64_t E, int V, int esz)
+{
+    const int piece = V * esz < 16 ? V * esz : 16;
+    return E % V == 0 && (uintptr_t)p % piece == 0 && ld * esz % piece == 0;
+}
+
+template <typename T> int route_typed(const RouteArgs &a, RouteShape r, bool wide, hipStream_t s)
+{
+    if (r.L == 16) {
+        switch (r.V) {
+        case 1: return launch_route<T, 16, 1>(a, wide, s);
+        case 2: return launch_route<T, 16, 2>(a, wide, s);
+        case 4: return launch_route<T, 16, 4>(a, wide, s);
+        case 8: return launch_route<T, 16, 8>(a, wide, s);
+        default: return launch_route<T, 16, 16>(a, wide, s);
+        }
+    }
+    switch (r.V) {
+    case 1: return launch_route<T, 64, 1>(a, wide, s);
+    case 2: return launch_route<T, 64, 2>(a, wide, s);
+    case 4: return launch_route<T, 64, 4>(a, wide, s);
+    case 8: return launch_route<T, 64, 8>(a, wide, s);
+    default: return launch_route<T, 64, 16>(a, wide, s);
+    }
+}
+template <typename T> int backward_typed(const RouteBackwardArgs &a, RouteShape r, bool wide, hipStream_t s)
+{
+    if (r.L == 16) {
+        switch (r.V) {
+        case 1: return launch_backward<T, 16, 1>(a, wide, s);
+        case 2: return launch_backward<T, 16, 2>(a, wide, s);
+        case 4: return launch_backward<T, 16, 4>(a, wide, s);
+        case 8: return launch_backward<T, 16, 8>(a, wide, s);
+        default: return launch_backward<T, 16, 16>(a, wide, s);
+        }
+    }
+    switch (r.V) {
+    case 1: return launch_backward<T, 64, 1>(a, wide, s);
+    case 2: return launch_backward<T, 64, 2>(a, wide, s);
+    case 4: return launch_backward<T, 64, 4>(a, wide, s);
+    case 8: return launch_backward<T, 64, 8>(a, wide, s);
+    default: return launch_backward<T, 64, 16>(a, wide, s);
+    }
+}
+
+int check_routing(int elem, int64_t tokens, int64_t experts, int64_t &ld, int score, int64_t top_k)
+{
+    if (!valid_elem(elem) || tokens < 0 || experts < 1 || ld < 0 || (score != GEMM_SCORE_SOFTMAX && score != GEMM_SCORE_SIGMOID) ||
+        top_k < 1 || top_k > experts)
+        return GEMM_ERR_INVALID_ARG;
+    if (!fill_ld(GEMM_ROW_MAJOR, ld, tokens, experts)) return GEMM_ERR_INVALID_ARG;
+    if (tokens > kMaxExtent || experts > GEMM_ROUTE_MAX_EXPERTS || top_k > GEMM_ROUTE_MAX_TOP_K || too_far(tokens, ld)) return GEMM_ERR_UNSUPPORTED;
+    return GEMM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gemm_route(int elem, int64_t tokens, int64_t experts, const void *logits, int64_t ld, const float *bias, int score,
+               int64_t groups, int64_t top_groups, int group_top, int64_t top_k, int renormalise, float scale,
+               float *weights, int32_t *indices, void *hip_stream)
+{
+    const int rc = check_routing(elem, tokens, experts, ld, score, top_k);
+    if (rc == GEMM_ERR_INVALID_ARG) return rc;
+    if (groups < 1 || experts % groups != 0 || top_groups < 1 || top_groups > groups || (group_top != 1 && group_top != 2) ||
+        top_k > top_groups * (experts / groups))
+        return GEMM_ERR_INVALID_ARG;
+    if (rc != GEMM_OK) return rc;
+    if (groups > GEMM_ROUTE_MAX_GROUPS) return GEMM_ERR_UNSUPPORTED;
+    if (tokens == 0) return GEMM_OK;
+    if (logits == nullptr || weights == nullptr || indices == nullptr) return GEMM_ERR_INVALID_ARG;
+    const RouteShape r = route_shape(experts, groups, top_k);
+    const int size = (int)(experts / groups), lanes = size / r.V;
+    RouteArgs a = {logits, bias, weights, indices, tokens, ld, (int)experts, (int)groups, (int)top_groups, group_top, size, (int)top_k,
+                   score == GEMM_SCORE_SOFTMAX, renormalise != 0, scale, divisor(size), 0};
+    if (size % r.V == 0 && lanes > 0 && (lanes & (lanes - 1)) == 0) a.lanes_per_group = lanes;
+    const bool wide = lanes_wide(logits, ld, experts, r.V, elem == GEMM_ELEM_F32 ? 4 : 2);
+    const hipStream_t s = (hipStream_t)hip_stream;
+    if (elem == GEMM_ELEM_F32) return route_typed<float>(a, r, wide, s);
+    return elem == GEMM_ELEM_F16 ? route_typed<_Float16>(a, r, wide, s) : route_typed<__bf16>(a, r, wide, s);
+}
+
+int gemm_route_backward(int elem, int64_t tokens, int64_t experts, const void *logits, int64_t ld, int score,
+                        int64_t top_k, int renormalise, float scale, const int32_t *indices, const float *d_weights,
+                        void *d_logits, int64_t ld_d, void *hip_stream)
+{
+    const int rc = check_routing(elem, tokens, experts, ld, score, top_k);
+    if (rc == GEMM_ERR_INVALID_ARG) return rc;
+    if (ld_d < 0 || !fill_ld(GEMM_ROW_MAJOR, ld_d, tokens, experts)) return GEMM_ERR_INVALID_ARG;
+    if (rc != GEMM_OK) return rc;
+    if (too_far(tokens, ld_d)) return GEMM_ERR_UNSUPPORTED;
+    if (tokens == 0) return GEMM_OK;
+    if (logits == nullptr || indices == nullptr || d_weights == nullptr || d_logits == nullptr) return GEMM_ERR_INVALID_ARG;
+    const RouteShape r = route_shape(experts, 1, top_k);
+    const RouteBackwardArgs a = {logits, indices, d_weights, d_logits, tokens, ld, ld_d, (int)experts, (int)top_k,
+                                 score == GEMM_SCORE_SOFTMAX, renormalise != 0, scale};
+    const int esz = elem == GEMM_ELEM_F32 ? 4 : 2;
+    const bool wide = lanes_wide(logits, ld, experts, r.V, esz) && lanes_wide(d_logits, ld_d, experts, r.V, esz);
+    const hipStream_t s = (hipStream_t)hip_stream;
+    if (elem == GEMM_ELEM_F32) return backward_typed<float>(a, r, wide, s);
+    return elem == GEMM_ELEM_F16 ? backward_typed<_Float16>(a, r, wide, s) : backward_typed<__bf16>(a, r, wide, s);
+}
+
+int gemm_route_plan(int64_t tokens, int64_t top_k, int64_t experts, const int32_t *indices, int32_t *offsets,
+                    int32_t *token_of, int32_t *slot_of, void *hip_stream)
+{
+    if (tokens < 0 || top_k < 1 || experts < 1 || offsets == nullptr) return GEMM_ERR_INVALID_ARG;
+    if (experts > GEMM_ROUTE_MAX_EXPERTS || tokens > kMaxEntries || top_k > kMaxEntries || tokens * top_k > kMaxEntries) return GEMM_ERR_UNSUPPORTED;
+    if (tokens > 0 && (indices == nullptr || token_of == nullptr || slot_of == nullptr)) return GEMM_ERR_INVALID_ARG;
+    return no_throw([&]() -> int {
+        const hipStream_t s = (hipStream_t)hip_stream;
+        const int64_t entries = tokens * top_k;
+        // Two launches cost 2 us more than one; a workgroup takes 1024 entries a step and half a microsecond for each.
+        const int64_t steps_all = ceil_div(entries, PLAN_THREADS);
+        int steps = (int)(steps_all > 0 ? steps_all : 1);
+        int blocks = 1;
+        if (steps_all > 8) {
+            steps = (int)(steps_all / 64 > 4 ? ceil_div(steps_all, 64) : 4);
+            blocks = (int)ceil_div(steps_all, steps);
+        }
+        PlanArgs a = {indices, offsets, token_of, slot_of, nullptr, entries, (int)experts, steps, 0, divisor(top_k)};
+        while ((1 << a.bits) < a.E) ++a.bits;
+        StreamScratch scratch;
+        if (blocks > 1) {
+            const int rc = stream_scratch(s, (size_t)blocks * experts * sizeof(int32_t), scratch);
+            if (rc != GEMM_OK) return rc;
+            a.counts = (int32_t *)scratch.ptr;
+            void *argv[] = {&a};
+            if (hipLaunchKernel((const void *)plan_count_kernel, dim3(blocks), dim3(PLAN_THREADS), argv, experts * sizeof(int), s) != hipSuccess) return GEMM_ERR_HIP;
+        }
+        void *argv[] = {&a};
+        const size_t lds = (PLAN_WAVES * experts + PLAN_WAVES) * sizeof(int);
+        return hipLaunchKernel((const void *)plan_place_kernel, dim3(blocks), dim3(PLAN_THREADS), argv, lds, s) == hipSuccess ? GEMM_OK : GEMM_ERR_HIP;
+    });
+}
+
+}  // extern "C"

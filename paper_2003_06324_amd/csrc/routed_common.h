@@ -1,0 +1,123 @@
+// What the kernels and entry points of gemm_routed.h share.
+#pragma once
+#include "gemm_kernel.h"
+#include "gemm_routed.h"
+
+#include <mutex>
+#include <tuple>
+#include <utility>
+
+namespace gemm_gfx950 {
+
+// A stream's workspace (the one that K-sliced products use), held for as long as launches that use it are being enqueued: another
+// host thread on the same stream may not put its own launches between them, and may replace the workspace by a larger one.
+// ptr is null if nothing was asked for.
+struct StreamScratch {
+    std::unique_lock<std::mutex> lock;
+    void *ptr = nullptr;
+    int num_cu = 0;
+};
+// bytes: how much is needed, 0 if only num_cu is asked for.  GEMM_ERR_WORKSPACE where the stream is being captured and its
+// workspace would have to grow.  (gemm_api.hip)
+int stream_scratch(hipStream_t stream, size_t bytes, StreamScratch &out);
+
+template <typename Tuple, size_t... I> static inline void routed_argv(void **argv, Tuple &vals, std::index_sequence<I...>)
+{
+    ((argv[I] = (void *)&std::get<I>(vals)), ...);
+}
+// Enqueues one kernel; the status is this launch's alone.  A launch has less than 2^32 threads in a dimension.
+template <typename... Params, typename... Args>
+static inline int enqueue(void (*kernel)(Params...), dim3 grid, dim3 block, hipStream_t s, Args... args)
+{
+    if ((uint64_t)grid.x * block.x > 0xffffffffull || grid.y > 65535) return GEMM_ERR_UNSUPPORTED;
+    std::tuple<Params...> vals(args...);
+    void *argv[sizeof...(Params)];
+    routed_argv(argv, vals, std::index_sequence_for<Params...>());
+    return hipLaunchKernel((const void *)kernel, grid, block, argv, 0, s) == hipSuccess ? GEMM_OK : GEMM_ERR_HIP;
+}
+
+// Nothing that C++ throws leaves a C entry (a mutex or a map may).
+template <typename F> static inline int no_throw(F f)
+{
+    try {
+        return f();
+    } catch (...) {
+        return GEMM_ERR_WORKSPACE;
+    }
+}
+
+constexpr int64_t kMaxExtent = 2147483647LL - 256;  // of every size, as in gemm.h
+
+static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+static inline bool valid_layout(int l) { return l == GEMM_ROW_MAJOR || l == GEMM_COL_MAJOR; }
+// ld of a rows x cols matrix: 0 becomes packed; false if it is too small
+static inline bool fill_ld(int layout, int64_t &ld, int64_t rows, int64_t cols)
+{
+    const int64_t packed = layout == GEMM_ROW_MAJOR ? cols : rows;
+    if (ld == 0) ld = packed;
+    return ld >= packed;
+}
+// elements from a matrix's first to behind its last one
+static inline int64_t extent_of(int layout, int64_t ld, int64_t rows, int64_t cols)
+{
+    if (rows == 0 || cols == 0) return 0;
+    return layout == GEMM_ROW_MAJOR ? (rows - 1) * ld + cols : (cols - 1) * ld + rows;
+}
+// base + count * stride elements stay within what 64-bit byte offsets can say
+static inline bool too_far(int64_t count, int64_t stride) { return stride > 0 && count > (INT64_MAX / 16) / stride; }
+
+static inline int elem_of_kind(int kind)
+{
+    return kind == GEMM_KIND_F32 ? GEMM_ELEM_F32 : (kind == GEMM_KIND_F16F32 || kind == GEMM_KIND_F16F16 ? GEMM_ELEM_F16 : GEMM_ELEM_BF16);
+}
+static inline bool valid_kind(int kind) { return kind >= GEMM_KIND_F32 && kind <= GEMM_KIND_BF16BF16; }
+static inline bool out16_of_kind(int kind) { return kind == GEMM_KIND_F16F16 || kind == GEMM_KIND_BF16BF16; }
+static inline bool valid_elem(int elem) { return elem >= GEMM_ELEM_F32 && elem <= GEMM_ELEM_BF16; }
+
+// Behind a store of 16 bytes: it may read its data registers up to two issue slots late, so nothing that is to be written to them
+// stands there, on whichever way the code goes on.
+__device__ __forceinline__ void behind_wide_store() { asm volatile("s_nop 1" ::: "memory"); }
+
+// One rounding to 16 bits, to nearest even (NaN stays NaN: both are instructions of gfx950, or what the compiler makes of a cast).
+template <typename T> __device__ __forceinline__ T rounded(float v) { return (T)v; }
+
+// ---------------------------------------------------------------------------
+// Reductions over the L lanes that share a token (16, a row of the data-parallel primitives, or a whole wave).  Every lane gets the
+// result; the order of the additions is the same for every lane.
+// ---------------------------------------------------------------------------
+template <int CTRL> __device__ __forceinline__ uint32_t lanes_moved(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+// partner of step s: quad pairs, quad halves, the other quad of eight lanes, the other eight of sixteen, then whole rows
+template <int S> __device__ __forceinline__ uint32_t partner(uint32_t v)
+{
+    if constexpr (S == 0) return lanes_moved<0xB1>(v);
+    else if constexpr (S == 1) return lanes_moved<0x4E>(v);
+    else if constexpr (S == 2) return lanes_moved<0x141>(v);
+    else if constexpr (S == 3) return lanes_moved<0x140>(v);
+    else return (uint32_t)__shfl_xor((int)v, S == 4 ? 16 : 32);
+}
+template <int L, int S = 0, typename F> __device__ __forceinline__ uint32_t over_lanes(uint32_t v, const F &f)
+{
+    if constexpr ((1 << S) >= L) return v;
+    else return over_lanes<L, S + 1>(f(v, partner<S>(v)), f);
+}
+template <int L> __device__ __forceinline__ float max_over(float v)
+{
+    return __uint_as_float(over_lanes<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+template <int L> __device__ __forceinline__ float sum_over(float v)
+{
+    return __uint_as_float(over_lanes<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+template <int L> __device__ __forceinline__ uint32_t umax_over(uint32_t v)
+{
+    return over_lanes<L>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int L> __device__ __forceinline__ uint32_t umin_over(uint32_t v)
+{
+    return over_lanes<L>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
+}  // namespace gemm_gfx950

@@ -1,0 +1,330 @@
+// Tiles of products whose rows choose their right operand: finding a tile's group, the K loop, the store.
+//
+// The LDS images, swizzles, direct loads and matrix instructions are those of gemm_kernel.h and gemm_stage_kernel.h.  What differs:
+// a tile belongs to a group of rows whose number only the device knows, rows of A may be gathered (a row's address is a lane's
+// offset anyway, so that costs nothing), and the loads' ranges always end with the operand (rows out of range, and what lies
+// past K, read as zeros).
+#pragma once
+#include "gemm_stage_kernel.h"
+#include "routed_common.h"
+
+namespace gemm_gfx950 {
+
+constexpr uint32_t NO_ROW = 0x80000000u;  // an offset past every range: loads of it bring zeros
+
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int scan_wave(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // one lane further in the row of sixteen
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // last lane of a row to the next row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+    return v;
+}
+
+// A group's rows, as far as they are rows
+struct Span { int lo, hi; };
+__device__ __forceinline__ Span group_span(const int32_t *offsets, int g, int rows)
+{
+    int lo = offsets[g], hi = offsets[g + 1];
+    lo = lo < 0 ? 0 : (lo > rows ? rows : lo);
+    hi = hi < lo ? lo : (hi > rows ? rows : hi);
+    return Span{lo, hi};
+}
+
+struct GroupTile { int group, lo, hi, tile_m, tile_n; };
+// The tile of this workgroup.  Tiles are numbered group by group, in a group column by column of tiles (those of one share the
+// group's matrix); every XCD gets one contiguous run.  Which group a number falls into, every wave adds up for itself:
+// the counts of 64 groups are one load and a scan.
+template <int BM> __device__ __forceinline__ bool group_tile(const int32_t *offsets, int groups, int rows, int tiles_n, int lane, GroupTile &out)
+{
+    int total = 0;
+    for (int c = 0; c < groups; c += 64) {
+        const int g = c + lane;
+        int n = 0;
+        if (g < groups) {
+            const Span s = group_span(offsets, g, rows);
+            n = (s.hi - s.lo + BM - 1) / BM;
+        }
+        total += __builtin_amdgcn_readlane(scan_wave(n), 63);
+    }
+    const uint32_t tiles = (uint32_t)total * (uint32_t)tiles_n;
+    const uint32_t per_xcd = (tiles + 7) / 8, i = blockIdx.x >> 3;
+    const uint32_t w = (blockIdx.x & 7) * per_xcd + i;
+    if (i >= per_xcd || w >= tiles) return false;
+    int before = 0;
+    for (int c = 0; c < groups; c += 64) {
+        const int g = c + lane;
+        int n = 0;
+        Span s = {0, 0};
+        if (g < groups) {
+            s = group_span(offsets, g, rows);
+            n = (s.hi - s.lo + BM - 1) / BM;
+        }
+        const int upto = before + scan_wave(n);
+        const uint64_t past = __ballot((uint32_t)upto * (uint32_t)tiles_n > w);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            const int count = __builtin_amdgcn_readlane(n, at);
+            const uint32_t local = w - (uint32_t)(__builtin_amdgcn_readlane(upto, at) - count) * (uint32_t)tiles_n;
+            out.group = c + at;
+            out.lo = __builtin_amdgcn_readlane(s.lo, at);
+            out.hi = __builtin_amdgcn_readlane(s.hi, at);
+            out.tile_n = __builtin_amdgcn_readfirstlane((int)(local / (uint32_t)count));
+            out.tile_m = __builtin_amdgcn_readfirstlane((int)(local - (uint32_t)out.tile_n * (uint32_t)count));
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// Direct loads of A: R rows from row0 on of the group whose first row is lo, gathered where there is a map.  The map's offsets
+// are 32 bits from A's beginning (the host sees to it), other rows' from the tile's first.
+template <typename T, int R, int NW> struct RowsLoader : StageLoader<T, R, NW, true> {
+    typedef StageLoader<T, R, NW, true> base_t;
+    __device__ __forceinline__ void init_rows(const T *A, int64_t lda, int a_rows, const int32_t *map, int lo, int hi, int row0, int K, int wave, int lane)
+    {
+        if (map == nullptr) {
+            // rows past A's last one read as zeros
+            const int there = a_rows < hi ? a_rows : hi;
+            if (lo + row0 < there) {
+                this->init(A + (int64_t)lo * lda, lda, row0, there - lo, K, 0, wave, lane);
+                if (there < hi) mask_rows(there - lo - row0, wave, lane);
+            } else {
+                this->init(A, lda, 0, 1, K, 0, wave, lane);
+                mask_rows(0, wave, lane);
+            }
+            return;
+        }
+        this->init(A, lda, 0, a_rows, K, 0, wave, lane);
+#pragma unroll
+        for (int i = 0; i < base_t::PER_WAVE; ++i) {
+            const int r = base_t::ROWS_PER_LOAD * (wave * base_t::PER_WAVE + i) + lane / GPR;
+            const int row = lo + row0 + r < hi ? map[lo + row0 + r] : -1;
+            const uint32_t at = (uint32_t)row * (uint32_t)(lda * (int64_t)sizeof(T)) + (uint32_t)(((lane % GPR) ^ swz_kc(r)) * 16);
+            this->off[i] = row >= 0 && row < a_rows ? at + base_t::LEAD - i % base_t::GROUP * 1024 : NO_ROW;
+        }
+    }
+    // rows of the tile from `first` on are zeros
+    __device__ __forceinline__ void mask_rows(int first, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < base_t::PER_WAVE; ++i)
+            if (base_t::ROWS_PER_LOAD * (wave * base_t::PER_WAVE + i) + lane / GPR >= first) this->off[i] = NO_ROW;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// The K loop on direct loads: NST stages of both operands in LDS, loads NST - 1 slabs ahead of their use.  Per slab: wait until it
+// has landed (a counted wait), one barrier (by which every wave has read the slab before, so its stage is free), the loads of the slab
+// NST - 1 further, the slab's fragments and matrix instructions.  The caller's at(h) points the loaders to slab h.
+// ---------------------------------------------------------------------------
+template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BKC> struct TileLoop {
+    static constexpr int NW = WM * WN, NT = NW * 64;
+    static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
+    static constexpr int A_BYTES = BM * RBK, B_BYTES = BN * RBK, STAGE = A_BYTES + B_BYTES, LDS_BYTES = NST * STAGE;
+    static constexpr int BK = Elem<T>::BK, KG = Elem<T>::KG, EPC = Elem<T>::EPC;
+    typedef typename Frag<T>::type frag_t;
+    typedef StageLoader<T, BM, NW, AKC> LoaderA;
+    typedef StageLoader<T, BN, NW, BKC> LoaderB;
+    static constexpr int NVA = LoaderA::PER_WAVE, NVB = LoaderB::PER_WAVE, NL = NVA + NVB;
+    static_assert((NST - 1) * NL <= 63, "the counted waits go up to 63 loads");
+
+    static __device__ __forceinline__ void zero(float16_t (&acc)[FM][FN])
+    {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    }
+
+    // One slab from the images at sA and sB: k-groups up to krem; `part`: the granule that holds krem - 1 is masked behind it
+    // (where an operand's own loads have not done so, that is, for K-contiguous ones).
+    static __device__ __forceinline__ void multiply(const GEMM_LDS(char) * sA, const GEMM_LDS(char) * sB, float16_t (&acc)[FM][FN], int wave, int lane)
+    {
+        const int wm = wave / WN, wn = wave % WN;
+#pragma unroll
+        for (int kg = 0; kg < KGS; ++kg) {
+            frag_t fa[FM], fb[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fa[i] = Fetch<T, BM, AKC>::get(sA, wm * TM + i * 32, kg, lane);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[j] = Fetch<T, BN, BKC>::get(sB, wn * TN + j * 32, kg, lane);
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) mma(acc[i][j], fa[i], fb[j]);
+        }
+    }
+    static __device__ __forceinline__ void multiply_last(const GEMM_LDS(char) * sA, const GEMM_LDS(char) * sB, float16_t (&acc)[FM][FN], int krem, int wave, int lane)
+    {
+        const int wm = wave / WN, wn = wave % WN;
+        const int part = krem % EPC, half = krem % KG / EPC;
+        uint4_t mask;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int in = part * (int)sizeof(T) - 4 * w;  // bytes of this word inside K
+            const uint32_t keep = in >= 4 ? 0xffffffffu : (in == 2 ? 0x0000ffffu : 0u);
+            mask[w] = part != 0 && (lane >> 5) == half ? keep : 0xffffffffu;
+        }
+#pragma unroll
+        for (int kg = 0; kg < KGS; ++kg) {
+            if (kg * KG >= krem) break;
+            frag_t fa[FM], fb[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                fa[i] = Fetch<T, BM, AKC>::get(sA, wm * TM + i * 32, kg, lane);
+                if (AKC && kg == krem / KG) fa[i] = __builtin_bit_cast(frag_t, __builtin_bit_cast(uint4_t, fa[i]) & mask);
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                fb[j] = Fetch<T, BN, BKC>::get(sB, wn * TN + j * 32, kg, lane);
+                if (BKC && kg == krem / KG) fb[j] = __builtin_bit_cast(frag_t, __builtin_bit_cast(uint4_t, fb[j]) & mask);
+            }
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) mma(acc[i][j], fa[i], fb[j]);
+        }
+    }
+
+    // n slabs, krem k in the last one.  Ends with every load landed; waves may still be reading LDS.
+    template <typename At>
+    static __device__ __forceinline__ void run(LoaderA &la, LoaderB &lb, const At &at, int n, int krem, GEMM_LDS(char) * lds, float16_t (&acc)[FM][FN],
+                                               int wave, int lane)
+    {
+        const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+        const uint32_t dst_a = lds0 + wave * (NVA * 1024), dst_b = lds0 + A_BYTES + wave * (NVB * 1024);
+        auto load = [&](int slot) {
+#pragma unroll
+            for (int q = 0; q < NVA; ++q) la.issue(dst_a + slot, q);
+#pragma unroll
+            for (int q = 0; q < NVB; ++q) lb.issue(dst_b + slot, q);
+        };
+#pragma unroll 1
+        for (int h = 0; h < NST - 1 && h < n; ++h) {
+            at(h);
+            load(h * STAGE);
+        }
+        int here = 0, free = (NST - 1) * STAGE;
+        for (int t = 0; t < n; ++t) {
+            wait_slabs_left<NST - 2, NL>(n - 1 - t);
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));  // own reads of the slab before are done
+            barrier_keep_loads();
+            if (t + NST - 1 < n) {
+                at(t + NST - 1);
+                load(free);
+            }
+            const GEMM_LDS(char) *s = lds + here;
+            if (t < n - 1 || krem == BK) multiply(s, s + A_BYTES, acc, wave, lane);
+            else multiply_last(s, s + A_BYTES, acc, krem, wave, lane);
+            free = here;
+            here = here == (NST - 1) * STAGE ? 0 : here + STAGE;
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Accumulators to rows of C.  Each wave puts 32 rows at a time into a piece of LDS of its own, as binary32, and writes them out in
+// pieces of 16 bytes a lane.  C: the tile's first element; rows, cols: what of the tile is stored.
+// ---------------------------------------------------------------------------
+template <typename TC, int BM, int BN, int WM, int WN, int LDS_BYTES>
+__device__ __forceinline__ void store_rows(const float16_t (&acc)[BM / WM / 32][BN / WN / 32], GEMM_LDS(char) * lds, TC *C, int64_t ldc, int rows, int cols,
+                                           int wave, int lane)
+{
+    constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
+    constexpr int SW = TN + 8;                  // words of a staged row: the two rows a write covers are in different halves of the banks
+    constexpr int EL = 16 / (int)sizeof(TC);    // elements of a piece
+    constexpr int LPR = TN / EL, RPI = 64 / LPR;
+    static_assert(64 % LPR == 0 && 32 % RPI == 0, "wave tile width");
+    static_assert(WM * WN * 32 * SW * 4 <= LDS_BYTES, "staging area");
+    typedef TC vec_t __attribute__((ext_vector_type(EL)));
+    typedef vec_t loose_t __attribute__((aligned(sizeof(TC))));
+    const int wm = wave / WN, wn = wave % WN;
+    GEMM_LDS(float) *stage = (GEMM_LDS(float) *)(lds + wave * (32 * SW * 4));
+    const int lrow = 4 * (lane >> 5), lcol = lane & 31;
+    const int srow = lane / LPR, col = wn * TN + lane % LPR * EL;
+    __syncthreads();  // every wave has read its last operands
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) stage[(8 * (r >> 2) + (r & 3) + lrow) * SW + j * 32 + lcol] = acc[i][j][r];
+#pragma unroll
+        for (int it = 0; it < 32 / RPI; ++it) {
+            const int row = wm * TM + i * 32 + it * RPI + srow;
+            const GEMM_LDS(float) *src = stage + (it * RPI + srow) * SW + lane % LPR * EL;
+            vec_t v;
+#pragma unroll
+            for (int x = 0; x < EL; ++x) v[x] = rounded<TC>(src[x]);
+            if (row >= rows) continue;
+            TC *dst = C + (int64_t)row * ldc + col;
+            if (col + EL <= cols) {
+                *(loose_t *)dst = v;
+                behind_wide_store();
+            } else {
+#pragma unroll
+                for (int x = 0; x < EL; ++x)
+                    if (col + x < cols) dst[x] = v[x];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The K loop through registers, for operands that direct loads do not serve (rows in the middle of a 4-byte word, offsets beyond
+// 32 bits): one slab in LDS, the next one on its way in registers.  Granules inside the operand are one 16-byte load of element
+// alignment, those at its edges element by element.
+// ---------------------------------------------------------------------------
+template <typename T, int R, int NT, bool KC> struct GranuleLoader {
+    static constexpr int EPC = Elem<T>::EPC, BK = Elem<T>::BK, CPR = R / EPC;
+    static constexpr int ITERS = R * GPR / NT;
+    static_assert(R * GPR % NT == 0, "whole rounds");
+    typedef uint4_t loose_t __attribute__((aligned(2)));  // element alignment of the narrower type
+    uint4_t v[ITERS];
+
+    // row(x): pointer to the beginning of row x of the operand as it is stored (a tile row, or k-row), null where it is zeros;
+    // first: of the other direction; extent: of the other direction.  Slab from k0 on.
+    template <typename Row> __device__ __forceinline__ void fetch(const Row &row, int first, int extent, int k0, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const int q = tid + i * NT;
+            const T *p = row(KC ? q / GPR : k0 + q / CPR);
+            const int at = KC ? k0 + q % GPR * EPC : first + q % CPR * EPC;
+            const int valid = p == nullptr ? 0 : extent - at;
+            uint4_t w = {0u, 0u, 0u, 0u};
+            if (valid >= EPC) {
+                w = *(const loose_t *)(p + at);
+            } else if (valid > 0) {
+                T e[EPC];
+#pragma unroll
+                for (int x = 0; x < EPC; ++x) e[x] = x < valid ? p[at + x] : (T)0.0f;
+                __builtin_memcpy(&w, e, 16);
+            }
+            v[i] = w;
+        }
+    }
+    __device__ __forceinline__ void store(GEMM_LDS(char) * img, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const int q = tid + i * NT;
+            if (KC) {
+                const int r = q / GPR;
+                *(GEMM_LDS(uint4_t) *)(img + r * RBK + (((q % GPR) ^ swz_kc(r)) << 4)) = v[i];
+            } else {
+                const int kk = q / CPR;
+                *(GEMM_LDS(uint4_t) *)(img + kk * (CPR * 16) + (((q % CPR) ^ swz_mc<T, CPR>(kk)) << 4)) = v[i];
+            }
+        }
+    }
+};
+
+}  // namespace gemm_gfx950
