@@ -1,5 +1,6 @@
 // The experts' products: C(i,:) = A(row(i),:) * B_e, rows of a group after one another.
 #pragma once
+#include "routed_ring.h"
 #include "routed_tile.h"
 
 namespace gemm_gfx950 {
@@ -50,6 +51,29 @@ __global__ __launch_bounds__(WM *WN * 64) void grouped_kernel(const GroupedArgs 
     Loop::zero(acc);
     Loop::run(la, lb, at, n, krem, lds, acc, wave, lane);
     store_rows<TC, BM, BN, WM, WN, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)(g.lo + m0) * p.ldc + n0, p.ldc, g.hi - g.lo - m0, p.N - n0, wave, lane);
+}
+
+// Large tiles, on the operand ring.
+template <typename T, typename TC, int BM, int BN, bool BKC>
+__global__ __launch_bounds__(256) void grouped_ring_kernel(const GroupedArgs p)
+{
+    typedef RingLoop<T, BM, BN, 2, 2, true, BKC> Loop;
+    __shared__ __attribute__((aligned(1024))) char smem[Loop::LDS_BYTES];
+    GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    GroupTile g;
+    if (!group_tile<BM>(p.offsets, p.groups, p.rows, p.tiles_n, lane, g)) return;
+    const int m0 = g.tile_m * BM, n0 = g.tile_n * BN;
+    const int n = (p.K + Loop::BK - 1) / Loop::BK, krem = p.K - (n - 1) * Loop::BK;
+    RingRowsLoader<T, BM, 4> la;
+    RingLoader<T, BN, 4, BKC> lb;
+    const T *const B = (const T *)p.B + (int64_t)g.group * p.strideB;
+    la.init_rows((const T *)p.A, p.lda, p.a_rows, p.row_map, g.lo, g.hi, m0, p.K, wave, lane);
+    lb.init(B, p.ldb, n0, p.N, wave, lane);
+    const bool checked = krem < Loop::BK || lb.reaches_end(n0, p.N);
+    float16_t acc[Loop::FM][Loop::FN];
+    Loop::run(la, lb, la.end, DirectLoader<T, BN, 4, BKC>::end_of(B, p.ldb, p.N, p.K), checked, n, krem, lds, acc, wave, lane);
+    store_rows<TC, BM, BN, 2, 2, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)(g.lo + m0) * p.ldc + n0, p.ldc, g.hi - g.lo - m0, p.N - n0, wave, lane);
 }
 
 // The same through registers: any alignment, any leading dimension.

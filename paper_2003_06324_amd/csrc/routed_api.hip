@@ -11,6 +11,9 @@ ROUTED_FORMS(extern, _Float16, float)
 ROUTED_FORMS(extern, _Float16, _Float16)
 ROUTED_FORMS(extern, __bf16, float)
 ROUTED_FORMS(extern, __bf16, __bf16)
+ROUTED_TYPES(extern, float)
+ROUTED_TYPES(extern, _Float16)
+ROUTED_TYPES(extern, __bf16)
 }  // namespace gemm_gfx950
 
 namespace {
@@ -24,6 +27,27 @@ bool direct(const void *p, int64_t ld, int64_t stride, int64_t esz)
 }
 // whether gathered rows' offsets fit 32 bits (with what the loader adds to them)
 bool gathers(int64_t rows, int64_t ld, int64_t esz) { return ld * esz < (1LL << 31) && rows * (ld * esz) < (1LL << 31) - (1 << 16); }
+
+// CUs of the current device (of this part, if it cannot be asked: what is wrong then the launch will say)
+int64_t cu_count()
+{
+    StreamScratch state;
+    return no_throw([&]() { return stream_scratch(nullptr, 0, state); }) == GEMM_OK ? state.num_cu : 256;
+}
+
+// Tile of the experts' products.  Few rows a group: 32 x 128, whose stages keep more of the experts' matrices on their way (bfloat16, 64
+// matrices of 2048 x 2048, 8 rows each 104 us, with 128 x 128 tiles 125; 128 of 2048 x 1536, 4 rows each 135 and 144; from 24 rows on
+// the same or behind).  Otherwise 128 x 128, two workgroups a CU, or 256 x 256, one, by the rounds that the chip takes for the tiles that
+// there will be about (half a tile more than its rows a group): a round of the former is half the work in 0.6 of the
+// time, where K is short and the start and end of a tile weigh 0.52 (64 matrices of 2048 x 2048: 128 rows each 140 and 165 us, 256
+// 204 and 186, 1024 629 and 546; 16 of 1024 x 4096: 512 rows each 79 and 96, 1024 177 and 164).
+int grouped_form(int64_t groups, int64_t rows, int64_t N, int64_t K, int64_t num_cu)
+{
+    if (rows <= 16 * groups) return GROUPED_32x128;
+    const int64_t rows256 = (rows / 256 + (groups + 1) / 2) * ceil_div(N, 256), rows128 = (rows / 128 + (groups + 1) / 2) * ceil_div(N, 128);
+    const double of256 = (double)ceil_div(rows256, num_cu), of128 = (K <= 1024 ? 0.52 : 0.6) * (double)ceil_div(rows128, 2 * num_cu);
+    return of256 <= of128 ? GROUPED_256x256 : GROUPED_128x128;
+}
 
 template <typename F> int by_kind(int kind, const F &f)
 {
@@ -54,14 +78,13 @@ int gemm_grouped(int kind, int64_t groups, const int32_t *offsets, int64_t rows,
     if (too_far(groups, strideB)) return GEMM_ERR_UNSUPPORTED;
     if (groups == 0 || rows == 0 || N == 0) return GEMM_OK;
     if (offsets == nullptr || C == nullptr || (K > 0 && (B == nullptr || (a_rows > 0 && A == nullptr)))) return GEMM_ERR_INVALID_ARG;
-    const int64_t esz = elem_size(kind);
+    const int64_t esz = elem_size(kind), num_cu = cu_count();
     int form = GROUPED_ANY;
     int64_t BM = 64, BN = 64;
     if (direct(A, lda, 0, esz) && direct(B, ldb, strideB, esz) && (row_map == nullptr || gathers(a_rows, lda, esz))) {
-        const int64_t each = ceil_div(rows, groups);
-        form = each <= 32 ? GROUPED_32x128 : (each <= 64 ? GROUPED_64x128 : GROUPED_128x128);
-        BM = each <= 32 ? 32 : (each <= 64 ? 64 : 128);
-        BN = 128;
+        form = grouped_form(groups, rows, N, K, num_cu);
+        BM = form == GROUPED_32x128 ? 32 : (form == GROUPED_128x128 ? 128 : 256);
+        BN = form == GROUPED_256x256 ? 256 : 128;
     }
     const int64_t tiles_n = ceil_div(N, BN), grid = grouped_grid(groups, rows, BM, tiles_n);
     if (grid > (1LL << 24) - 1) return GEMM_ERR_UNSUPPORTED;
@@ -98,9 +121,8 @@ int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t
         std::swap(a.M, a.N);
     }
     const bool fast = direct(A, lda, 0, esz) && direct(D, ldd, 0, esz) && (row_map == nullptr || gathers(a_rows, lda, esz));
-    const int64_t edge = fast ? 128 : 64;
-    a.tiles_m = (int)ceil_div(a.M, edge);
-    a.tiles_n = (int)ceil_div(a.N, edge);
+    a.tiles_m = (int)ceil_div(a.M, fast ? 256 : 64);
+    a.tiles_n = (int)ceil_div(a.N, fast ? 128 : 64);
     const int64_t per = (int64_t)a.tiles_m * a.tiles_n;
     if (per > (1LL << 24) || per * groups > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)(8 * ceil_div(per * groups, 8)));
@@ -134,30 +156,70 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
     return no_throw([&]() -> int {
         const hipStream_t s = (hipStream_t)hip_stream;
         const int64_t esz = elem_size(kind);
-        AdaptersArgs a = {A, B, down, up, C, adapter_of, scales, nullptr, lda, ldb, ldc, ld_down, stride_down, ld_up, stride_up, (int)rows, (int)N, (int)K,
-                          some ? (int)adapters : 0, (int)rank, 0, 1, (int)K, layout_up == GEMM_COL_MAJOR, 0, 0, {}, {}};
+        const int elem = elem_of_kind(kind);
+        const bool bkc = layoutB == GEMM_COL_MAJOR, dkc = layout_down == GEMM_COL_MAJOR;
+        AdaptersArgs a = {};
+        a.A = A, a.B = B, a.down = down, a.up = up, a.C = C, a.adapter_of = adapter_of, a.scales = scales;
+        a.lda = lda, a.ldb = ldb, a.ldc = ldc, a.ld_down = ld_down, a.stride_down = stride_down, a.ld_up = ld_up, a.stride_up = stride_up;
+        a.rows = (int)rows, a.N = (int)N, a.K = (int)K, a.adapters = some ? (int)adapters : 0, a.rank = (int)rank;
+        a.up_kc = layout_up == GEMM_COL_MAJOR;
         const bool fast = direct(A, lda, 0, esz) && direct(B, ldb, 0, esz);
-        const int form = !fast ? ADAPTERS_ANY : (rows <= 256 ? ADAPTERS_32x128 : ADAPTERS_128x128);
-        const int64_t BM = form == ADAPTERS_ANY ? 64 : (form == ADAPTERS_32x128 ? 32 : 128), BN = form == ADAPTERS_ANY ? 64 : 128;
-        const int64_t tiles_m = ceil_div(rows, BM), tiles_n = ceil_div(N, BN);
-        if (tiles_m > (1LL << 24) || tiles_n > (1LL << 24) || tiles_m * tiles_n > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
         StreamScratch scratch;
-        if (some) {
-            const int64_t row_tiles = ceil_div(rows, DOWN_ROWS);
-            const int64_t turns = std::min<int64_t>(adapters, row_tiles >= 64 ? 1 : DOWN_ROWS);
-            a.t_pitch = (int)(ceil_div(rank, 32) * 32);
-            // K in slices while there are fewer workgroups than CUs, of at least 256 k
-            const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(1, row_tiles), ceil_div(K, 256)));
-            a.t_k = (int)(ceil_div(ceil_div(K, slices), 64) * 64);
-            a.t_splits = (int)ceil_div(K, a.t_k);
-            const int rc = stream_scratch(s, (size_t)a.t_splits * rows * a.t_pitch * sizeof(float), scratch);
+        const int state = stream_scratch(s, 0, scratch);
+        if (state != GEMM_OK) return state;
+        const int64_t num_cu = scratch.num_cu;
+        scratch.lock.unlock();
+        if (ceil_div(rows, 128) * ceil_div(N, 128) < num_cu / 2 && rows <= 65535) {
+            // few rows: tiles of 64 x 64, K in slices of at least 256 k while there are less than two workgroups a CU
+            a.tiles_m = (int)ceil_div(rows, 64);
+            a.tiles_n = (int)ceil_div(N, 64);
+            const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+            const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(2 * num_cu / tiles, K / 256));
+            a.k_slice = (int)std::max<int64_t>(64, ceil_div(ceil_div(K, slices), 64) * 64);
+            a.slices = (int)ceil_div(K, a.k_slice);
+            a.part_pitch = (int)(ceil_div(N, 32) * 32);
+            if (some) {
+                const int64_t row_tiles = ceil_div(rows, DOWN_ROWS);
+                a.turns = (int)std::min<int64_t>(adapters, DOWN_ROWS);
+                a.t_pitch = (int)(ceil_div(rank, 32) * 32);
+                const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(num_cu / std::max<int64_t>(1, row_tiles), ceil_div(K, 256)));
+                a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
+                a.t_slices = (int)ceil_div(K, a.t_k);
+                a.down_groups = (int)(row_tiles * a.t_slices * a.turns);
+            }
+            const size_t t_bytes = (size_t)a.t_slices * rows * a.t_pitch * sizeof(float);
+            const int rc = stream_scratch(s, t_bytes + (size_t)a.slices * rows * a.part_pitch * sizeof(float) + 256, scratch);
             if (rc != GEMM_OK) return rc;
-            a.t = (float *)scratch.ptr;
-            const dim3 grid((unsigned)(row_tiles * a.t_splits), (unsigned)turns);
-            const bool kc = layout_down == GEMM_COL_MAJOR;
-            const int sent = kind == GEMM_KIND_F32 ? launch_adapters_down<float>(kc, grid, s, a)
-                             : elem_of_kind(kind) == GEMM_ELEM_F16 ? launch_adapters_down<_Float16>(kc, grid, s, a)
-                                                                   : launch_adapters_down<__bf16>(kc, grid, s, a);
+            a.part = (float *)scratch.ptr;
+            a.t = a.part + (size_t)a.slices * rows * a.part_pitch;
+            const dim3 grid((unsigned)(a.down_groups + tiles * a.slices));
+            const int sent = grid.x == 0                ? GEMM_OK  // (K is zero)
+                             : elem == GEMM_ELEM_F32    ? launch_adapters_slices<float>(bkc, dkc, fast, grid, s, a)
+                             : elem == GEMM_ELEM_F16    ? launch_adapters_slices<_Float16>(bkc, dkc, fast, grid, s, a)
+                                                        : launch_adapters_slices<__bf16>(bkc, dkc, fast, grid, s, a);
+            if (sent != GEMM_OK) return sent;
+            const dim3 join((unsigned)rows, (unsigned)ceil_div(N, JOIN_COLS));
+            return by_kind(kind, [&](auto *t, auto *tc) {
+                return launch_adapters_join<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(join, s, a);
+            });
+        }
+        const int form = !fast ? ADAPTERS_ANY : (ceil_div(rows, 256) * ceil_div(N, 256) < num_cu ? ADAPTERS_128x128 : ADAPTERS_256x256);
+        const int64_t edge = form == ADAPTERS_ANY ? 64 : (form == ADAPTERS_128x128 ? 128 : 256);
+        const int64_t tiles_m = ceil_div(rows, edge), tiles_n = ceil_div(N, edge);
+        if (tiles_m > (1LL << 24) || tiles_n > (1LL << 24) || tiles_m * tiles_n > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
+        if (some) {
+            const int parts = elem == GEMM_ELEM_F32 ? 1 : (elem == GEMM_ELEM_F16 ? 2 : 3);
+            a.t_pitch = (int)(ceil_div(rank, 64) * 64);
+            const size_t part_bytes = (size_t)rows * parts * a.t_pitch * esz;
+            const int rc = stream_scratch(s, part_bytes + rows * sizeof(float), scratch);
+            if (rc != GEMM_OK) return rc;
+            a.t_parts = scratch.ptr;
+            a.t_scale = (float *)((char *)scratch.ptr + part_bytes);
+            const dim3 grid((unsigned)ceil_div(rows, DOWN_ROWS));
+            const bool fast_down = direct(A, lda, 0, esz) && direct(down, ld_down, stride_down, esz);
+            const int sent = elem == GEMM_ELEM_F32   ? launch_adapters_down<float>(dkc, fast_down, grid, s, a)
+                             : elem == GEMM_ELEM_F16 ? launch_adapters_down<_Float16>(dkc, fast_down, grid, s, a)
+                                                     : launch_adapters_down<__bf16>(dkc, fast_down, grid, s, a);
             if (sent != GEMM_OK) return sent;
         }
         a.tiles_m = (int)tiles_m;
@@ -166,7 +228,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         a.by_last_rows = divisor(tiles_m % GM > 0 ? tiles_m % GM : 1);
         const dim3 grid((unsigned)(8 * ceil_div(tiles_m * tiles_n, 8)));
         return by_kind(kind, [&](auto *t, auto *tc) {
-            return launch_adapters<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(form, layoutB == GEMM_COL_MAJOR, grid, s, a);
+            return launch_adapters<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(form, bkc, grid, s, a);
         });
     });
 }

@@ -7,14 +7,14 @@
 namespace gemm_gfx950 {
 
 // forms of grouped_kernel: rows and columns of a tile; 0: through registers
-enum { GROUPED_ANY = 0, GROUPED_32x128 = 1, GROUPED_64x128 = 2, GROUPED_128x128 = 3 };
+enum { GROUPED_ANY = 0, GROUPED_32x128 = 1, GROUPED_128x128 = 2, GROUPED_256x256 = 3 };
 
 template <typename T, typename TC, bool BKC> static int launch_grouped_form(int form, dim3 grid, hipStream_t s, const GroupedArgs &a)
 {
     switch (form) {
     case GROUPED_32x128: return enqueue(grouped_kernel<T, TC, 32, 128, 1, 4, 4, BKC>, grid, dim3(256), s, a);
-    case GROUPED_64x128: return enqueue(grouped_kernel<T, TC, 64, 128, 2, 2, 3, BKC>, grid, dim3(256), s, a);
-    case GROUPED_128x128: return enqueue(grouped_kernel<T, TC, 128, 128, 2, 2, 2, BKC>, grid, dim3(256), s, a);
+    case GROUPED_128x128: return enqueue(grouped_ring_kernel<T, TC, 128, 128, BKC>, grid, dim3(256), s, a);
+    case GROUPED_256x256: return enqueue(grouped_ring_kernel<T, TC, 256, 256, BKC>, grid, dim3(256), s, a);
     default: return enqueue(grouped_any_kernel<T, TC, 64, 64, BKC>, grid, dim3(256), s, a);
     }
 }
@@ -26,16 +26,17 @@ template <typename T, typename TC> int launch_grouped(int form, bool bkc, dim3 g
 enum { WGRAD_ANY = 0, WGRAD_128x128 = 1 };
 template <typename T, typename TC> int launch_wgrad(int form, dim3 grid, hipStream_t s, const WgradArgs &a)
 {
-    if (form == WGRAD_128x128) return enqueue(wgrad_kernel<T, TC, 128, 128, 2>, grid, dim3(256), s, a);
+    if (form == WGRAD_128x128) return enqueue(wgrad_kernel<T, TC, 256, 128, 4, 2, 3>, grid, dim3(512), s, a);
     return enqueue(wgrad_any_kernel<T, TC, 64, 64>, grid, dim3(256), s, a);
 }
 
-enum { ADAPTERS_ANY = 0, ADAPTERS_32x128 = 1, ADAPTERS_128x128 = 2 };
+// forms of the product of many rows
+enum { ADAPTERS_ANY = 0, ADAPTERS_128x128 = 1, ADAPTERS_256x256 = 2 };
 template <typename T, typename TC, bool BKC> static int launch_adapters_form(int form, dim3 grid, hipStream_t s, const AdaptersArgs &a)
 {
     switch (form) {
-    case ADAPTERS_32x128: return enqueue(adapters_kernel<T, TC, 32, 128, 1, 4, 4, BKC>, grid, dim3(256), s, a);
-    case ADAPTERS_128x128: return enqueue(adapters_kernel<T, TC, 128, 128, 2, 2, 2, BKC>, grid, dim3(256), s, a);
+    case ADAPTERS_128x128: return enqueue(adapters_ring_kernel<T, TC, 128, 128, BKC>, grid, dim3(256), s, a);
+    case ADAPTERS_256x256: return enqueue(adapters_ring_kernel<T, TC, 256, 256, BKC>, grid, dim3(256), s, a);
     default: return enqueue(adapters_any_kernel<T, TC, 64, 64, BKC>, grid, dim3(256), s, a);
     }
 }
@@ -43,14 +44,48 @@ template <typename T, typename TC> int launch_adapters(int form, bool bkc, dim3 
 {
     return bkc ? launch_adapters_form<T, TC, true>(form, grid, s, a) : launch_adapters_form<T, TC, false>(form, grid, s, a);
 }
-template <typename T> int launch_adapters_down(bool kc, dim3 grid, hipStream_t s, const AdaptersArgs &a)
+template <typename T, typename TC> int launch_adapters_join(dim3 grid, hipStream_t s, const AdaptersArgs &a)
 {
-    return kc ? enqueue(adapters_down_kernel<T, true>, grid, dim3(256), s, a) : enqueue(adapters_down_kernel<T, false>, grid, dim3(256), s, a);
+    return enqueue(adapters_join_kernel<T, TC>, grid, dim3(256), s, a);
 }
+
+// few rows: T and the product in slices
+template <typename T, int BM, int NST, bool BKC, bool DKC> static int launch_slices_direct(bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
+{
+    return direct ? enqueue(adapters_slices_kernel<T, BM, 64, NST, BKC, DKC, true>, grid, dim3(256), s, a)
+                  : enqueue(adapters_slices_kernel<T, 64, 64, 3, BKC, DKC, false>, grid, dim3(256), s, a);
+}
+template <typename T, int BM, int NST> static int launch_slices_form(bool bkc, bool dkc, bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
+{
+    if (bkc) return dkc ? launch_slices_direct<T, BM, NST, true, true>(direct, grid, s, a) : launch_slices_direct<T, BM, NST, true, false>(direct, grid, s, a);
+    return dkc ? launch_slices_direct<T, BM, NST, false, true>(direct, grid, s, a) : launch_slices_direct<T, BM, NST, false, false>(direct, grid, s, a);
+}
+template <typename T> int launch_adapters_slices(bool bkc, bool dkc, bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
+{
+    return launch_slices_form<T, 64, 5>(bkc, dkc, direct, grid, s, a);
+}
+
+// T of many rows
+template <typename T, bool KC> static int launch_down_form(bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
+{
+    if (!direct) return enqueue(adapters_down_any_kernel<T, KC>, grid, dim3(256), s, a);
+    if (a.rank <= 64) return enqueue(adapters_down_kernel<T, 64, 6, KC>, grid, dim3(256), s, a);
+    if (a.rank <= 128) return enqueue(adapters_down_kernel<T, 128, 4, KC>, grid, dim3(256), s, a);
+    return enqueue(adapters_down_kernel<T, 256, 4, KC>, grid, dim3(256), s, a);
+}
+template <typename T> int launch_adapters_down(bool kc, bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
+{
+    return kc ? launch_down_form<T, true>(direct, grid, s, a) : launch_down_form<T, false>(direct, grid, s, a);
+}
+
+#define ROUTED_TYPES(PREFIX, T)                                                                                    \
+    PREFIX template int launch_adapters_slices<T>(bool, bool, bool, dim3, hipStream_t, const AdaptersArgs &);       \
+    PREFIX template int launch_adapters_down<T>(bool, bool, dim3, hipStream_t, const AdaptersArgs &);
 
 #define ROUTED_FORMS(PREFIX, T, TC)                                                                        \
     PREFIX template int launch_grouped<T, TC>(int, bool, dim3, hipStream_t, const GroupedArgs &);           \
     PREFIX template int launch_wgrad<T, TC>(int, dim3, hipStream_t, const WgradArgs &);                     \
-    PREFIX template int launch_adapters<T, TC>(int, bool, dim3, hipStream_t, const AdaptersArgs &);
+    PREFIX template int launch_adapters<T, TC>(int, bool, dim3, hipStream_t, const AdaptersArgs &);         \
+    PREFIX template int launch_adapters_join<T, TC>(dim3, hipStream_t, const AdaptersArgs &);
 
 }  // namespace gemm_gfx950

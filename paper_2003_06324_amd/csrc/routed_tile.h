@@ -117,6 +117,13 @@ template <typename T, int R, int NW> struct RowsLoader : StageLoader<T, R, NW, t
     }
 };
 
+// Fetch with a k-group that is not a constant
+template <typename T, int R, bool KC> __device__ __forceinline__ typename Frag<T>::type fetch_group(const GEMM_LDS(char) * img, int r0, int kg, int lane)
+{
+    if constexpr (KC) return Fetch<T, R, true>::get(img, r0, kg, lane);
+    else return Fetch<T, R, false>::get(img + kg * (Elem<T>::KG * R * (int)sizeof(T)), r0, 0, lane);  // k-groups lie one behind the other
+}
+
 // ---------------------------------------------------------------------------
 // The K loop on direct loads: NST stages of both operands in LDS, loads NST - 1 slabs ahead of their use.  Per slab: wait until it
 // has landed (a counted wait), one barrier (by which every wave has read the slab before, so its stage is free), the loads of the slab
@@ -193,10 +200,9 @@ template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BK
         }
     }
 
-    // n slabs, krem k in the last one.  Ends with every load landed; waves may still be reading LDS.
-    template <typename At>
-    static __device__ __forceinline__ void run(LoaderA &la, LoaderB &lb, const At &at, int n, int krem, GEMM_LDS(char) * lds, float16_t (&acc)[FM][FN],
-                                               int wave, int lane)
+    // n slabs; multiply(image of A, image of B, last slab).  Ends with every load landed; waves may still be reading LDS.
+    template <typename At, typename Multiply>
+    static __device__ __forceinline__ void run_with(LoaderA &la, LoaderB &lb, const At &at, int n, GEMM_LDS(char) * lds, int wave, const Multiply &multiply)
     {
         const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
         const uint32_t dst_a = lds0 + wave * (NVA * 1024), dst_b = lds0 + A_BYTES + wave * (NVB * 1024);
@@ -220,12 +226,20 @@ template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BK
                 at(t + NST - 1);
                 load(free);
             }
-            const GEMM_LDS(char) *s = lds + here;
-            if (t < n - 1 || krem == BK) multiply(s, s + A_BYTES, acc, wave, lane);
-            else multiply_last(s, s + A_BYTES, acc, krem, wave, lane);
+            multiply(lds + here, lds + here + A_BYTES, t == n - 1);
             free = here;
             here = here == (NST - 1) * STAGE ? 0 : here + STAGE;
         }
+    }
+    // krem k in the last slab
+    template <typename At>
+    static __device__ __forceinline__ void run(LoaderA &la, LoaderB &lb, const At &at, int n, int krem, GEMM_LDS(char) * lds, float16_t (&acc)[FM][FN],
+                                               int wave, int lane)
+    {
+        run_with(la, lb, at, n, lds, wave, [&](const GEMM_LDS(char) * sA, const GEMM_LDS(char) * sB, bool last) {
+            if (!last || krem == BK) multiply(sA, sB, acc, wave, lane);
+            else multiply_last(sA, sB, acc, krem, wave, lane);
+        });
     }
 };
 
@@ -326,5 +340,33 @@ template <typename T, int R, int NT, bool KC> struct GranuleLoader {
         }
     }
 };
+
+// The whole K loop of rows m0 .. of A and columns n0 .. of B, k from k0 to k1, on two stages of LDS (a stage was read two slabs before
+// it is written again, and a barrier has been passed since).  rows, cols: of the matrices.
+template <typename T, typename Loop, int BM, int BN, bool BKC>
+__device__ __forceinline__ void granule_loop(const T *A, int64_t lda, const T *B, int64_t ldb, int m0, int rows, int n0, int cols, int k0, int k1,
+                                             GEMM_LDS(char) * lds, float16_t (&acc)[Loop::FM][Loop::FN], int tid, int wave, int lane)
+{
+    GranuleLoader<T, BM, Loop::NT, true> la;
+    GranuleLoader<T, BN, Loop::NT, BKC> lb;
+    auto fetch = [&](int k) {
+        la.fetch([&](int r) -> const T * { return m0 + r < rows ? A + (int64_t)(m0 + r) * lda : nullptr; }, 0, k1, k, tid);
+        lb.fetch([&](int r) -> const T * {
+            if (BKC) return n0 + r < cols ? B + (int64_t)(n0 + r) * ldb : nullptr;
+            return r < k1 ? B + (int64_t)r * ldb : nullptr;
+        }, n0, BKC ? k1 : cols, k, tid);
+    };
+    if (k0 < k1) fetch(k0);
+    int stage = 0;
+    for (int k = k0; k < k1; k += Loop::BK) {
+        la.store(lds + stage, tid);
+        lb.store(lds + stage + Loop::A_BYTES, tid);
+        if (k + Loop::BK < k1) fetch(k + Loop::BK);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
+        barrier_keep_loads();
+        Loop::multiply(lds + stage, lds + stage + Loop::A_BYTES, acc, wave, lane);
+        stage = Loop::STAGE - stage;
+    }
+}
 
 }  // namespace gemm_gfx950

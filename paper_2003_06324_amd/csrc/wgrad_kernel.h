@@ -60,10 +60,10 @@ __device__ __forceinline__ bool wgrad_tile(const WgradArgs &p, int &group, int &
     return true;
 }
 
-template <typename T, typename TC, int BM, int BN, int NST>
-__global__ __launch_bounds__(256) void wgrad_kernel(const WgradArgs p)
+template <typename T, typename TC, int BM, int BN, int WM, int WN, int NST>
+__global__ __launch_bounds__(WM *WN * 64) void wgrad_kernel(const WgradArgs p)
 {
-    typedef TileLoop<T, BM, BN, 2, 2, NST, false, false> Loop;
+    typedef TileLoop<T, BM, BN, WM, WN, NST, false, false> Loop;
     __shared__ __attribute__((aligned(1024))) char smem[Loop::LDS_BYTES];
     __shared__ int window_[MAP_WINDOW];
     GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
@@ -77,14 +77,14 @@ __global__ __launch_bounds__(256) void wgrad_kernel(const WgradArgs p)
     const int n = (count + Loop::BK - 1) / Loop::BK;
     const int32_t *const map = p.map_x != nullptr ? p.map_x : p.map_y;
 
-    KRowsLoader<T, BM, 4> lx;
-    KRowsLoader<T, BN, 4> ly;
+    KRowsLoader<T, BM, Loop::NW> lx;
+    KRowsLoader<T, BN, Loop::NW> ly;
     lx.init_rows((const T *)p.X, p.ldx, p.x_rows, p.map_x != nullptr, lo, hi, m0, p.M, wave, lane);
     ly.init_rows((const T *)p.Y, p.ldy, p.y_rows, p.map_y != nullptr, lo, hi, n0, p.N, wave, lane);
     auto at = [&](int h) {
         if (map != nullptr && h * Loop::BK % MAP_WINDOW == 0) {
             __syncthreads();  // the numbers before are done with
-            for (int i = tid; i < MAP_WINDOW; i += 256) window[i] = h * Loop::BK + i < count ? map[lo + h * Loop::BK + i] : -1;
+            for (int i = tid; i < MAP_WINDOW; i += Loop::NT) window[i] = h * Loop::BK + i < count ? map[lo + h * Loop::BK + i] : -1;
             __syncthreads();
         }
         if (p.map_x != nullptr) lx.gather(window, p.ldx, p.x_rows, m0, p.M, h * Loop::BK, count, wave, lane);
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void wgrad_kernel(const WgradArgs p)
     float16_t acc[Loop::FM][Loop::FN];
     Loop::zero(acc);
     Loop::run(lx, ly, at, n, Loop::BK, lds, acc, wave, lane);  // (rows past the last one are zeros)
-    store_rows<TC, BM, BN, 2, 2, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)group * p.strideC + (int64_t)m0 * p.ldc + n0, p.ldc, p.M - m0, p.N - n0, wave, lane);
+    store_rows<TC, BM, BN, WM, WN, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)group * p.strideC + (int64_t)m0 * p.ldc + n0, p.ldc, p.M - m0, p.N - n0, wave, lane);
 }
 
 // The same through registers: any alignment, any leading dimension.
