@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void adapters_slices_kernel(const AdaptersArgs
         };
         Loop::run(la, lb, at, n, krem, lds, acc, wave, lane);
     } else {
-        granule_loop<T, Loop, BM, BN, BKC>((const T *)p.A, p.lda, (const T *)p.B, p.ldb, m0, p.rows, n0, p.N, k0, k1, lds, acc, tid, wave, lane);
+        granule_product<T, Loop, BM, BN, BKC>((const T *)p.A, p.lda, (const T *)p.B, p.ldb, m0, p.rows, n0, p.N, k0, k1, lds, acc, tid, wave, lane);
     }
     store_rows<float, BM, BN, WM, WN, Loop::LDS_BYTES>(acc, lds, p.part + ((int64_t)slice * p.rows + m0) * p.part_pitch + n0, p.part_pitch, p.rows - m0, p.N - n0,
                                                        wave, lane);
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(256) void adapters_any_kernel(const AdaptersArgs p)
     const int m0 = tile_m * BM, n0 = tile_n * BN;
     float16_t acc[Loop::FM][Loop::FN];
     Loop::zero(acc);
-    granule_loop<T, Loop, BM, BN, BKC>((const T *)p.A, p.lda, (const T *)p.B, p.ldb, m0, p.rows, n0, p.N, 0, p.K, lds, acc, tid, wave, lane);
+    granule_product<T, Loop, BM, BN, BKC>((const T *)p.A, p.lda, (const T *)p.B, p.ldb, m0, p.rows, n0, p.N, 0, p.K, lds, acc, tid, wave, lane);
     add_and_store<T, TC, BM, BN, 2, 2, Loop::LDS_BYTES>(p, lds, acc, m0, n0, tid, wave, lane);
 }
 

@@ -99,26 +99,19 @@ __global__ __launch_bounds__(256) void grouped_any_kernel(const GroupedArgs p)
         if (BKC) return n0 + r < p.N ? B + (int64_t)(n0 + r) * p.ldb : nullptr;
         return r < p.K ? B + (int64_t)r * p.ldb : nullptr;
     };
-    GranuleLoader<T, BM, Loop::NT, true> la;
-    GranuleLoader<T, BN, Loop::NT, BKC> lb;
+    GranuleLoader<T, BM, Loop::NT, true> la[GRANULE_DEPTH];
+    GranuleLoader<T, BN, Loop::NT, BKC> lb[GRANULE_DEPTH];
     float16_t acc[Loop::FM][Loop::FN];
     Loop::zero(acc);
-    auto fetch = [&](int k0) {
-        la.fetch(row_a, 0, p.K, k0, tid);
-        lb.fetch(row_b, n0, BKC ? p.K : p.N, k0, tid);
+    auto fetch = [&](auto set, int k0) {
+        la[set].fetch(row_a, 0, p.K, k0, tid);
+        lb[set].fetch(row_b, n0, BKC ? p.K : p.N, k0, tid);
     };
-    if (p.K > 0) fetch(0);
-    int stage = 0;
-    for (int k0 = 0; k0 < p.K; k0 += Loop::BK) {
-        // (two stages: the one written here was read two slabs ago, and a barrier has been passed since)
-        la.store(lds + stage, tid);
-        lb.store(lds + stage + Loop::A_BYTES, tid);
-        if (k0 + Loop::BK < p.K) fetch(k0 + Loop::BK);
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
-        barrier_keep_loads();
-        Loop::multiply(lds + stage, lds + stage + Loop::A_BYTES, acc, wave, lane);
-        stage = Loop::STAGE - stage;
-    }
+    auto store = [&](auto set, int stage) {
+        la[set].store(lds + stage, tid);
+        lb[set].store(lds + stage + Loop::A_BYTES, tid);
+    };
+    granule_loop<Loop>(fetch, store, 0, p.K, lds, acc, wave, lane);
     store_rows<TC, BM, BN, 2, 2, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)(g.lo + m0) * p.ldc + n0, p.ldc, g.hi - g.lo - m0, p.N - n0, wave, lane);
 }
 

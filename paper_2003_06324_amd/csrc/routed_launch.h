@@ -23,10 +23,17 @@ template <typename T, typename TC> int launch_grouped(int form, bool bkc, dim3 g
     return bkc ? launch_grouped_form<T, TC, true>(form, grid, s, a) : launch_grouped_form<T, TC, false>(form, grid, s, a);
 }
 
-enum { WGRAD_ANY = 0, WGRAD_128x128 = 1 };
+enum { WGRAD_ANY = 0, WGRAD_128x128 = 1, WGRAD_256x256 = 2 };
+template <typename T, typename TC, int E> static int launch_wgrad_ring(dim3 grid, hipStream_t s, const WgradArgs &a)
+{
+    if (a.map_x != nullptr) return enqueue(wgrad_kernel<T, TC, E, E, 1>, grid, dim3(256), s, a);
+    if (a.map_y != nullptr) return enqueue(wgrad_kernel<T, TC, E, E, 2>, grid, dim3(256), s, a);
+    return enqueue(wgrad_kernel<T, TC, E, E, 0>, grid, dim3(256), s, a);
+}
 template <typename T, typename TC> int launch_wgrad(int form, dim3 grid, hipStream_t s, const WgradArgs &a)
 {
-    if (form == WGRAD_128x128) return enqueue(wgrad_kernel<T, TC, 256, 128, 4, 2, 3>, grid, dim3(512), s, a);
+    if (form == WGRAD_128x128) return launch_wgrad_ring<T, TC, 128>(grid, s, a);
+    if (form == WGRAD_256x256) return launch_wgrad_ring<T, TC, 256>(grid, s, a);
     return enqueue(wgrad_any_kernel<T, TC, 64, 64>, grid, dim3(256), s, a);
 }
 

@@ -70,6 +70,7 @@ template <typename T, int R, int NW, bool KC> struct RingLoader {
         asm volatile("s_add_i32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
                      : : "s"(wave_lds), "i"(OFF + i * 1024), "v"(off[i]), "s"(rsrc) : "memory", "m0", "scc");
     }
+    __device__ __forceinline__ void prefetch() {}  // what the next advance() will need
     __device__ __forceinline__ void advance(bool more)
     {
         const uint64_t to = base() + (more ? step : 0);
@@ -205,6 +206,8 @@ template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC> struct
             } else {
                 y_advance(h / 2 + 1 < n);
                 y_at(h / 2 + 1);
+                la.prefetch();
+                lb.prefetch();
             }
         }
         zero_acc();
@@ -225,6 +228,8 @@ template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC> struct
             kgroup(fa[1], fb[1], fa[0], fb[0], cA, cB, 2, true, load_x_hi, std::integral_constant<int, NVX - NVX / 2>());
             x_advance(more);
             if constexpr (decltype(near_end)::value) x_at(h);
+            la.prefetch();
+            lb.prefetch();
             kgroup(fa[0], fb[0], fa[1], fb[1], cA, cB, 3, true, no_load, L0());
             __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(NVX));  // the next slab landed, own reads of this one done
             barrier_keep_loads();

@@ -245,11 +245,11 @@ template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BK
 
 // ---------------------------------------------------------------------------
 // Accumulators to rows of C.  Each wave puts 32 rows at a time into a piece of LDS of its own, as binary32, and writes them out in
-// pieces of 16 bytes a lane.  C: the tile's first element; rows, cols: what of the tile is stored.
+// pieces of 16 bytes a lane.  C: the tile's first element; rows, cols: what of the tile is stored; stream: past the L2.
 // ---------------------------------------------------------------------------
 template <typename TC, int BM, int BN, int WM, int WN, int LDS_BYTES>
 __device__ __forceinline__ void store_rows(const float16_t (&acc)[BM / WM / 32][BN / WN / 32], GEMM_LDS(char) * lds, TC *C, int64_t ldc, int rows, int cols,
-                                           int wave, int lane)
+                                           int wave, int lane, bool stream = false)
 {
     constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     constexpr int SW = TN + 8;                  // words of a staged row: the two rows a write covers are in different halves of the banks
@@ -280,7 +280,8 @@ __device__ __forceinline__ void store_rows(const float16_t (&acc)[BM / WM / 32][
             if (row >= rows) continue;
             TC *dst = C + (int64_t)row * ldc + col;
             if (col + EL <= cols) {
-                *(loose_t *)dst = v;
+                if (stream) __builtin_nontemporal_store(v, (loose_t *)dst);
+                else *(loose_t *)dst = v;
                 behind_wide_store();
             } else {
 #pragma unroll
@@ -302,9 +303,11 @@ template <typename T, int R, int NT, bool KC> struct GranuleLoader {
     static_assert(R * GPR % NT == 0, "whole rounds");
     typedef uint4_t loose_t __attribute__((aligned(2)));  // element alignment of the narrower type
     uint4_t v[ITERS];
+    int late[ITERS];  // bits that a granule's elements lie behind its beginning
 
     // row(x): pointer to the beginning of row x of the operand as it is stored (a tile row, or k-row), null where it is zeros;
     // first: of the other direction; extent: of the other direction.  Slab from k0 on.
+    // A granule over the operand's edge is loaded as the last 16 bytes of its row, and moved into place when it is stored.
     template <typename Row> __device__ __forceinline__ void fetch(const Row &row, int first, int extent, int k0, int tid)
     {
 #pragma unroll
@@ -314,19 +317,36 @@ template <typename T, int R, int NT, bool KC> struct GranuleLoader {
             const int at = KC ? k0 + q % GPR * EPC : first + q % CPR * EPC;
             const int valid = p == nullptr ? 0 : extent - at;
             uint4_t w = {0u, 0u, 0u, 0u};
-            if (valid >= EPC) {
-                w = *(const loose_t *)(p + at);
+            late[i] = valid < EPC && valid > 0 ? (EPC - valid) * 8 * (int)sizeof(T) : 0;
+            if (__builtin_expect(extent >= EPC, 1)) {
+                if (valid > 0) w = *(const loose_t *)(p + (valid < EPC ? extent - EPC : at));
             } else if (valid > 0) {
-                T e[EPC];
+                T e[EPC];  // (a row shorter than a granule)
 #pragma unroll
                 for (int x = 0; x < EPC; ++x) e[x] = x < valid ? p[at + x] : (T)0.0f;
                 __builtin_memcpy(&w, e, 16);
+                late[i] = 0;
             }
             v[i] = w;
         }
     }
-    __device__ __forceinline__ void store(GEMM_LDS(char) * img, int tid) const
+    __device__ __forceinline__ void settle()
     {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) any |= late[i] != 0;
+        if (__ballot(any) == 0) return;
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const uint64_t lo = ((uint64_t)v[i][1] << 32) | v[i][0], hi = ((uint64_t)v[i][3] << 32) | v[i][2];
+            const int s = late[i];
+            const uint64_t l = s == 0 ? lo : (s >= 64 ? hi >> (s - 64) : (lo >> s) | (hi << (64 - s))), h = s >= 64 ? 0 : hi >> s;
+            v[i] = uint4_t{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+        }
+    }
+    __device__ __forceinline__ void store(GEMM_LDS(char) * img, int tid)
+    {
+        settle();
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {
             const int q = tid + i * NT;
@@ -341,32 +361,56 @@ template <typename T, int R, int NT, bool KC> struct GranuleLoader {
     }
 };
 
-// The whole K loop of rows m0 .. of A and columns n0 .. of B, k from k0 to k1, on two stages of LDS (a stage was read two slabs before
-// it is written again, and a barrier has been passed since).  rows, cols: of the matrices.
-template <typename T, typename Loop, int BM, int BN, bool BKC>
-__device__ __forceinline__ void granule_loop(const T *A, int64_t lda, const T *B, int64_t ldb, int m0, int rows, int n0, int cols, int k0, int k1,
-                                             GEMM_LDS(char) * lds, float16_t (&acc)[Loop::FM][Loop::FN], int tid, int wave, int lane)
+// The K loop through registers, k from k0 to k1: DEPTH slabs on their way in register sets of their own (a slab is multiplied in a fraction of
+// a memory round trip), two stages of LDS (one was read two slabs before it is written again, and a barrier has been
+// passed since).  fetch(set, k), store(set, stage): a slab to registers, from there to LDS; set is a constant.
+constexpr int GRANULE_DEPTH = 3;
+template <typename Loop, typename Fetch_, typename Store_>
+__device__ __forceinline__ void granule_loop(const Fetch_ &fetch, const Store_ &store, int k0, int k1, GEMM_LDS(char) * lds, float16_t (&acc)[Loop::FM][Loop::FN],
+                                             int wave, int lane)
 {
-    GranuleLoader<T, BM, Loop::NT, true> la;
-    GranuleLoader<T, BN, Loop::NT, BKC> lb;
-    auto fetch = [&](int k) {
-        la.fetch([&](int r) -> const T * { return m0 + r < rows ? A + (int64_t)(m0 + r) * lda : nullptr; }, 0, k1, k, tid);
-        lb.fetch([&](int r) -> const T * {
-            if (BKC) return n0 + r < cols ? B + (int64_t)(n0 + r) * ldb : nullptr;
-            return r < k1 ? B + (int64_t)r * ldb : nullptr;
-        }, n0, BKC ? k1 : cols, k, tid);
-    };
-    if (k0 < k1) fetch(k0);
+    static_assert(GRANULE_DEPTH == 3, "the sets below");
+    typedef std::integral_constant<int, 0> S0;
+    typedef std::integral_constant<int, 1> S1;
+    typedef std::integral_constant<int, 2> S2;
+    constexpr int BK = Loop::BK;
+    if (k0 < k1) fetch(S0(), k0);
+    if (k0 + BK < k1) fetch(S1(), k0 + BK);
+    if (k0 + 2 * BK < k1) fetch(S2(), k0 + 2 * BK);
     int stage = 0;
-    for (int k = k0; k < k1; k += Loop::BK) {
-        la.store(lds + stage, tid);
-        lb.store(lds + stage + Loop::A_BYTES, tid);
-        if (k + Loop::BK < k1) fetch(k + Loop::BK);
+    auto slab = [&](auto set, int k) {
+        store(set, stage);
+        if (k + GRANULE_DEPTH * BK < k1) fetch(set, k + GRANULE_DEPTH * BK);
         __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
         barrier_keep_loads();
         Loop::multiply(lds + stage, lds + stage + Loop::A_BYTES, acc, wave, lane);
         stage = Loop::STAGE - stage;
+    };
+    for (int k = k0; k < k1; k += GRANULE_DEPTH * BK) {
+        slab(S0(), k);
+        if (k + BK < k1) slab(S1(), k + BK);
+        if (k + 2 * BK < k1) slab(S2(), k + 2 * BK);
     }
+}
+// the same of rows m0 .. of A and columns n0 .. of B; rows, cols: of the matrices
+template <typename T, typename Loop, int BM, int BN, bool BKC>
+__device__ __forceinline__ void granule_product(const T *A, int64_t lda, const T *B, int64_t ldb, int m0, int rows, int n0, int cols, int k0, int k1,
+                                                GEMM_LDS(char) * lds, float16_t (&acc)[Loop::FM][Loop::FN], int tid, int wave, int lane)
+{
+    GranuleLoader<T, BM, Loop::NT, true> la[GRANULE_DEPTH];
+    GranuleLoader<T, BN, Loop::NT, BKC> lb[GRANULE_DEPTH];
+    auto fetch = [&](auto set, int k) {
+        la[set].fetch([&](int r) -> const T * { return m0 + r < rows ? A + (int64_t)(m0 + r) * lda : nullptr; }, 0, k1, k, tid);
+        lb[set].fetch([&](int r) -> const T * {
+            if (BKC) return n0 + r < cols ? B + (int64_t)(n0 + r) * ldb : nullptr;
+            return r < k1 ? B + (int64_t)r * ldb : nullptr;
+        }, n0, BKC ? k1 : cols, k, tid);
+    };
+    auto store = [&](auto set, int stage) {
+        la[set].store(lds + stage, tid);
+        lb[set].store(lds + stage + Loop::A_BYTES, tid);
+    };
+    granule_loop<Loop>(fetch, store, k0, k1, lds, acc, wave, lane);
 }
 
 }  // namespace gemm_gfx950

@@ -1,5 +1,6 @@
 // Gradients of the experts' matrices: C_e = sum over the group's rows of X(i,:)^T * Y(i,:).
 #pragma once
+#include "routed_ring.h"
 #include "routed_tile.h"
 
 namespace gemm_gfx950 {
@@ -10,94 +11,201 @@ struct WgradArgs {
     const int32_t *offsets, *map_x, *map_y;  // (one of the maps at most)
     int64_t ldx, ldy, ldc, strideC;
     int groups, rows, x_rows, y_rows, M, N, tiles_m, tiles_n;
+    int stream;  // C is stored past the L2
 };
 
-constexpr int MAP_WINDOW = 4096;  // row numbers of a group kept in LDS
+// Direct loads of an operand whose k-rows are a group's rows.  Without a map its base moves from slab to slab.  With one the lanes' offsets
+// are set anew for every slab: a wave's rows are neighbours in the map, so their numbers are scalar loads, one slab ahead, and
+// cost the vector unit a selection and an addition for each load.
+template <typename T, int R, int NW, bool MAPPED> struct RingKRowsLoader : RingLoader<T, R, NW, false> {
+    typedef RingLoader<T, R, NW, false> base_t;
+    static constexpr int CPR = base_t::CPR, PER_WAVE = base_t::PER_WAVE, BK = base_t::BK, EPC = base_t::EPC;
+    static constexpr int RPL = 64 / CPR, ROWS = PER_WAVE * RPL;  // k-rows of a load, of a wave
+    static_assert(64 % CPR == 0 && ROWS * NW == BK && ROWS % 4 == 0, "whole k-rows");
+    typedef const __attribute__((address_space(4))) uint32_t *numbers_t;
+    uint64_t end;
+    const int32_t *map;   // the whole map
+    int at, rows;         // entry of it that `next` begins with, and their number
+    uint32_t there, ldb;  // rows of the operand, bytes between them (all of them below 2^31)
+    uint32_t next[MAPPED ? ROWS : 1];
+    uint32_t col[2];      // the lane's place in its row, of the two swizzles that its loads have
 
-// Direct loads of an operand whose k-rows are a group's rows.  Without a map its base moves from slab to slab; with one the lanes'
-// offsets are set anew for every slab, from row numbers in LDS.
-template <typename T, int R, int NW> struct KRowsLoader : StageLoader<T, R, NW, false> {
-    typedef StageLoader<T, R, NW, false> base_t;
-    __device__ __forceinline__ void init_rows(const T *X, int64_t ld, int there, bool mapped, int lo, int hi, int col0, int cols, int wave, int lane)
+    static constexpr int swizzle_of(int i) { return RPL == 4 ? 0 : (sizeof(T) == 2 ? i & 1 : (i * RPL >> 2) & 1); }
+
+    // map_, rows_: the map of all groups, and how many entries it has (at least BK)
+    __device__ __forceinline__ void init_rows(const T *X, int64_t ld, int rows_there, const int32_t *map_, int rows_, int lo, int hi, int col0, int cols, int wave,
+                                              int lane)
     {
-        const int last = mapped ? there : (there < hi ? there : hi) - lo;  // rows from the origin on
-        this->init(mapped ? X : X + (int64_t)lo * ld, ld, col0, cols, last > 0 ? last : 1, 0, wave, lane);
-        if (last <= 0) this->no_rows();
+        typedef DirectLoader<T, R, NW, false> ends_t;
+        if constexpr (!MAPPED) {
+            const T *const first = X + (int64_t)lo * ld;
+            this->init(first, ld, col0, cols, wave, lane);
+            end = hi > lo ? ends_t::end_of(first, ld, cols, hi - lo) : 0;
+        } else {
+            this->init(X, ld, col0, cols, wave, lane);
+            there = (uint32_t)rows_there;
+            end = there > 0 ? ends_t::end_of(X, ld, cols, rows_there) : 0;
+            map = map_;
+            rows = rows_;
+            ldb = (uint32_t)(ld * (int64_t)sizeof(T));
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int i = x == 0 || RPL == 4 ? 0 : (sizeof(T) == 2 ? 1 : 4 / RPL);  // a load with that swizzle
+                const int kk = i * RPL + lane / CPR;
+                const int m = ((lane % CPR) ^ swz_mc<T, CPR>(kk)) * EPC;
+                col[x] = (uint32_t)((col0 + m < cols ? m : 0) * (int)sizeof(T));
+            }
+            // any slab may hold the operand's last row: the range always ends with the operand (its base stays)
+            base_t::last_slab(end, BK, wave, lane);
+            at = lo + wave * ROWS;
+            numbers();
+            offsets(lane);
+            at += BK;
+            numbers();
+        }
     }
-    __device__ __forceinline__ void no_rows() { this->end = 0; }
-    // the range ends with the operand's rows, of which there may be none left (rows of the group behind A's last one)
-    __device__ __forceinline__ void range()
+    // Rows behind the group's last one are other groups', or, at the map's end, any: rows_until() sees to them.
+    __device__ __forceinline__ void numbers()
     {
-        const uint64_t base = ((uint64_t)(uint32_t)this->rsrc[1] << 32) | (uint32_t)this->rsrc[0];
-        if (base >= this->end) this->no_range();
-        else this->exact_range();
+        const numbers_t m = (numbers_t)(uintptr_t)(map + (at < rows - ROWS ? at : rows - ROWS));
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) next[r] = m[r];
     }
-    // slab from k-row k on; window: the row numbers in LDS, from a multiple of MAP_WINDOW
-    __device__ __forceinline__ void gather(const GEMM_LDS(int) * window, int64_t ld, int there, int col0, int cols, int k, int count, int wave, int lane)
+    __device__ __forceinline__ void offsets(int lane)
     {
 #pragma unroll
-        for (int i = 0; i < base_t::PER_WAVE; ++i) {
-            const int q = 64 * (wave * base_t::PER_WAVE + i) + lane;
-            const int kk = q / base_t::CPR;
-            const int m = ((q % base_t::CPR) ^ swz_mc<T, base_t::CPR>(kk)) * base_t::EPC;
-            const int row = window[(k + kk) & (MAP_WINDOW - 1)];
-            const uint32_t at = (uint32_t)row * (uint32_t)(ld * (int64_t)sizeof(T)) + (uint32_t)((col0 + m < cols ? m : 0) * (int)sizeof(T));
-            this->off[i] = k + kk < count && row >= 0 && row < there ? at + base_t::LEAD - i % base_t::GROUP * 1024 : NO_ROW;
+        for (int i = 0; i < PER_WAVE; ++i) {
+            uint32_t row[RPL];
+#pragma unroll
+            for (int x = 0; x < RPL; ++x) {
+                // a number that names no row becomes the one behind the last, which the loads' range leaves out
+                const uint32_t r = next[i * RPL + x];
+                row[x] = (r < there ? r : there) * ldb;
+            }
+            uint32_t mine = row[0];
+#pragma unroll
+            for (int x = 1; x < RPL; ++x) mine = lane / CPR == x ? row[x] : mine;
+            this->off[i] = mine + col[swizzle_of(i)];
+        }
+    }
+    // The slab whose first row is entry `first` of the map has `count` rows: the others are zeros, and the window of numbers may have been
+    // moved back from the map's end, so the lanes ask for theirs themselves.
+    __device__ __forceinline__ void rows_until(int count, int first, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < PER_WAVE; ++i) {
+            const int kk = wave * ROWS + i * RPL + lane / CPR;
+            uint32_t r = there;
+            if (kk < count) {
+                r = (uint32_t)map[first + kk];
+                r = r < there ? r : there;
+            }
+            this->off[i] = kk < count ? r * ldb + col[swizzle_of(i)] : NO_ROW;
+        }
+    }
+    __device__ __forceinline__ void last_slab(uint64_t to, int krem, int wave, int lane)
+    {
+        if constexpr (!MAPPED) {
+            base_t::last_slab(to, krem, wave, lane);
+        } else if (krem < BK) {  // (offsets() has moved on already)
+            rows_until(krem, at - BK - wave * ROWS, wave, lane);
+        }
+    }
+    // The numbers for the next advance().  The fragments' reads are waited for first: with scalar loads on their way every wait of
+    // either kind is one for all of them, and the next one is the barrier's, a k-group from here.
+    __device__ __forceinline__ void prefetch()
+    {
+        if constexpr (MAPPED) {
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
+            numbers();
+        }
+    }
+    __device__ __forceinline__ void advance(bool more)
+    {
+        if constexpr (!MAPPED) {
+            base_t::advance(more);
+        } else if (more) {
+            offsets(threadIdx.x & 63);
+            at += BK;
         }
     }
 };
 
-// tile of this workgroup: matrix by matrix, every XCD one contiguous run
-__device__ __forceinline__ bool wgrad_tile(const WgradArgs &p, int &group, int &tile_m, int &tile_n)
+// What a tile's start and store weigh, in slabs of 64 rows.
+constexpr int WGRAD_TILE = 8;
+// workgroups of a launch: as many tiles as can fall into an eighth of the weight, for each XCD
+static inline int64_t wgrad_grid(int64_t groups, int64_t rows, int64_t per)
 {
-    const uint32_t per = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n, tiles = per * (uint32_t)p.groups, per_xcd = (tiles + 7) / 8;
-    const uint32_t i = blockIdx.x >> 3, w = (blockIdx.x & 7) * per_xcd + i;
-    if (i >= per_xcd || w >= tiles) return false;
-    group = (int)(w / per);
-    const uint32_t in = w - (uint32_t)group * per;
-    tile_n = (int)(in / (uint32_t)p.tiles_m);
-    tile_m = (int)(in - (uint32_t)tile_n * (uint32_t)p.tiles_m);
-    return true;
+    const int64_t weight = per * (rows / 64 + groups * (1 + WGRAD_TILE));  // at most
+    const int64_t most = ceil_div(ceil_div(weight, 8), WGRAD_TILE) + 1;
+    return 8 * (most < per * groups ? most : per * groups);
+}
+// Tile of this workgroup.  Tiles are numbered matrix by matrix and take as long as their group has rows, so the XCDs get contiguous runs of
+// the same weight, not of the same number.
+__device__ __forceinline__ bool wgrad_tile(const WgradArgs &p, int lane, int &group, int &tile_m, int &tile_n)
+{
+    const uint32_t per = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
+    auto weight_of = [&](int g) {  // of one tile
+        if (g >= p.groups) return 0;
+        const Span s = group_span(p.offsets, g, p.rows);
+        return (s.hi - s.lo + 63) / 64 + WGRAD_TILE;
+    };
+    int total = 0;
+    for (int c = 0; c < p.groups; c += 64) total += __builtin_amdgcn_readlane(scan_wave(weight_of(c + lane)), 63);
+    // the tiles whose beginnings lie in [from, to) of the weight; the i-th of them
+    const uint64_t all = (uint64_t)(uint32_t)total * per, share = (all + 7) / 8;
+    const uint64_t from = share * (blockIdx.x & 7), to = from + share;
+    uint32_t i = blockIdx.x >> 3;
+    uint64_t before = 0;
+    for (int c = 0; c < p.groups; c += 64) {
+        const int w = weight_of(c + lane);
+        const int upto = scan_wave(w);
+        const uint64_t begin = before + (uint64_t)(uint32_t)(upto - w) * per, end = before + (uint64_t)(uint32_t)upto * per;
+        // this lane's group: its tiles [first, last) are the XCD's
+        uint32_t first = 0, last = 0;
+        if (w > 0 && begin < to && end > from) {
+            first = begin >= from ? 0 : (uint32_t)((from - begin + w - 1) / w);
+            last = end <= to ? per : (uint32_t)((to - begin + w - 1) / w);
+        }
+        const int mine = last > first ? (int)(last - first) : 0;
+        const int sum = scan_wave(mine);
+        const uint64_t past = __ballot((uint32_t)sum > i);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            group = c + at;
+            const uint32_t in = i - (uint32_t)(__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at)) + (uint32_t)__builtin_amdgcn_readlane((int)first, at);
+            tile_n = __builtin_amdgcn_readfirstlane((int)(in / (uint32_t)p.tiles_m));
+            tile_m = __builtin_amdgcn_readfirstlane((int)(in - (uint32_t)tile_n * (uint32_t)p.tiles_m));
+            return true;
+        }
+        i -= (uint32_t)__builtin_amdgcn_readlane(sum, 63);
+        before += (uint64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * per;
+    }
+    return false;
 }
 
-template <typename T, typename TC, int BM, int BN, int WM, int WN, int NST>
-__global__ __launch_bounds__(WM *WN * 64) void wgrad_kernel(const WgradArgs p)
+// MAPPED: 0 no map, 1 X's rows are gathered, 2 Y's
+template <typename T, typename TC, int BM, int BN, int MAPPED>
+__global__ __launch_bounds__(256) void wgrad_kernel(const WgradArgs p)
 {
-    typedef TileLoop<T, BM, BN, WM, WN, NST, false, false> Loop;
+    typedef RingLoop<T, BM, BN, 2, 2, false, false> Loop;
     __shared__ __attribute__((aligned(1024))) char smem[Loop::LDS_BYTES];
-    __shared__ int window_[MAP_WINDOW];
     GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
-    GEMM_LDS(int) *window = (GEMM_LDS(int) *)window_;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int group, tile_m, tile_n;
-    if (!wgrad_tile(p, group, tile_m, tile_n)) return;
+    if (!wgrad_tile(p, lane, group, tile_m, tile_n)) return;
     const Span s = group_span(p.offsets, group, p.rows);
     const int lo = __builtin_amdgcn_readfirstlane(s.lo), hi = __builtin_amdgcn_readfirstlane(s.hi);
     const int m0 = tile_m * BM, n0 = tile_n * BN, count = hi - lo;
-    const int n = (count + Loop::BK - 1) / Loop::BK;
-    const int32_t *const map = p.map_x != nullptr ? p.map_x : p.map_y;
-
-    KRowsLoader<T, BM, Loop::NW> lx;
-    KRowsLoader<T, BN, Loop::NW> ly;
-    lx.init_rows((const T *)p.X, p.ldx, p.x_rows, p.map_x != nullptr, lo, hi, m0, p.M, wave, lane);
-    ly.init_rows((const T *)p.Y, p.ldy, p.y_rows, p.map_y != nullptr, lo, hi, n0, p.N, wave, lane);
-    auto at = [&](int h) {
-        if (map != nullptr && h * Loop::BK % MAP_WINDOW == 0) {
-            __syncthreads();  // the numbers before are done with
-            for (int i = tid; i < MAP_WINDOW; i += Loop::NT) window[i] = h * Loop::BK + i < count ? map[lo + h * Loop::BK + i] : -1;
-            __syncthreads();
-        }
-        if (p.map_x != nullptr) lx.gather(window, p.ldx, p.x_rows, m0, p.M, h * Loop::BK, count, wave, lane);
-        else if (h > 0) lx.advance();
-        if (p.map_y != nullptr) ly.gather(window, p.ldy, p.y_rows, n0, p.N, h * Loop::BK, count, wave, lane);
-        else if (h > 0) ly.advance();
-        lx.range();
-        ly.range();
-    };
+    const int n = (count + Loop::BK - 1) / Loop::BK, krem = count - (n - 1) * Loop::BK;
+    RingKRowsLoader<T, BM, 4, MAPPED == 1> lx;
+    RingKRowsLoader<T, BN, 4, MAPPED == 2> ly;
+    lx.init_rows((const T *)p.X, p.ldx, p.x_rows, p.map_x, p.rows, lo, hi, m0, p.M, wave, lane);
+    ly.init_rows((const T *)p.Y, p.ldy, p.y_rows, p.map_y, p.rows, lo, hi, n0, p.N, wave, lane);
+    const bool checked = krem < Loop::BK || lx.reaches_end(m0, p.M) || ly.reaches_end(n0, p.N);
     float16_t acc[Loop::FM][Loop::FN];
-    Loop::zero(acc);
-    Loop::run(lx, ly, at, n, Loop::BK, lds, acc, wave, lane);  // (rows past the last one are zeros)
-    store_rows<TC, BM, BN, WM, WN, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)group * p.strideC + (int64_t)m0 * p.ldc + n0, p.ldc, p.M - m0, p.N - n0, wave, lane);
+    Loop::run(lx, ly, lx.end, ly.end, checked, n, krem, lds, acc, wave, lane);
+    store_rows<TC, BM, BN, 2, 2, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)group * p.strideC + (int64_t)m0 * p.ldc + n0, p.ldc, p.M - m0, p.N - n0, wave, lane, p.stream != 0);
 }
 
 // The same through registers: any alignment, any leading dimension.
@@ -109,7 +217,7 @@ __global__ __launch_bounds__(256) void wgrad_any_kernel(const WgradArgs p)
     GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int group, tile_m, tile_n;
-    if (!wgrad_tile(p, group, tile_m, tile_n)) return;
+    if (!wgrad_tile(p, lane, group, tile_m, tile_n)) return;
     const Span s = group_span(p.offsets, group, p.rows);
     const int lo = __builtin_amdgcn_readfirstlane(s.lo), hi = __builtin_amdgcn_readfirstlane(s.hi);
     const int m0 = tile_m * BM, n0 = tile_n * BN, count = hi - lo;
@@ -120,26 +228,20 @@ __global__ __launch_bounds__(256) void wgrad_any_kernel(const WgradArgs p)
     };
     auto row_x = [&](int k) { return row_of((const T *)p.X, p.ldx, p.map_x, p.x_rows, k); };
     auto row_y = [&](int k) { return row_of((const T *)p.Y, p.ldy, p.map_y, p.y_rows, k); };
-    GranuleLoader<T, BM, Loop::NT, false> lx;
-    GranuleLoader<T, BN, Loop::NT, false> ly;
+    GranuleLoader<T, BM, Loop::NT, false> lx[GRANULE_DEPTH];
+    GranuleLoader<T, BN, Loop::NT, false> ly[GRANULE_DEPTH];
     float16_t acc[Loop::FM][Loop::FN];
     Loop::zero(acc);
-    auto fetch = [&](int k0) {
-        lx.fetch(row_x, m0, p.M, k0, tid);
-        ly.fetch(row_y, n0, p.N, k0, tid);
+    auto fetch = [&](auto set, int k0) {
+        lx[set].fetch(row_x, m0, p.M, k0, tid);
+        ly[set].fetch(row_y, n0, p.N, k0, tid);
     };
-    if (count > 0) fetch(0);
-    int stage = 0;
-    for (int k0 = 0; k0 < count; k0 += Loop::BK) {
-        lx.store(lds + stage, tid);
-        ly.store(lds + stage + Loop::A_BYTES, tid);
-        if (k0 + Loop::BK < count) fetch(k0 + Loop::BK);
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
-        barrier_keep_loads();
-        Loop::multiply(lds + stage, lds + stage + Loop::A_BYTES, acc, wave, lane);
-        stage = Loop::STAGE - stage;
-    }
-    store_rows<TC, BM, BN, 2, 2, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)group * p.strideC + (int64_t)m0 * p.ldc + n0, p.ldc, p.M - m0, p.N - n0, wave, lane);
+    auto store = [&](auto set, int stage) {
+        lx[set].store(lds + stage, tid);
+        ly[set].store(lds + stage + Loop::A_BYTES, tid);
+    };
+    granule_loop<Loop>(fetch, store, 0, count, lds, acc, wave, lane);
+    store_rows<TC, BM, BN, 2, 2, Loop::LDS_BYTES>(acc, lds, (TC *)p.C + (int64_t)group * p.strideC + (int64_t)m0 * p.ldc + n0, p.ldc, p.M - m0, p.N - n0, wave, lane, p.stream != 0);
 }
 
 }  // namespace gemm_gfx950
