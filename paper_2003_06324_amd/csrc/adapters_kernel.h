@@ -3,8 +3,8 @@
 // With T(i,:) = scale_a A(i,:) down_a, rows x rank, held in binary32:
 //   few rows:  one launch computes T and the shared product, both in slices of K (a few rows would not give every CU
 //              work otherwise), and a second one adds up the slices, multiplies T with the up matrices and rounds;
-//   many rows: a first launch computes T, a second one is the shared product, whose tiles, when their K loop is done,
-//              multiply their rows of T with the up matrices of the adapters that the tile has.  There T is cut
+//   many rows: a first launch computes T in slices of K, a second one adds them up, a third one is the shared product, whose
+//              tiles, when their K loop is done, multiply their rows of T with the up matrices of the adapters that the tile has.  There T is cut
 //              into 16-bit parts for the matrix instructions: three of bfloat16, or two of binary16 relative to the row's largest
 //              element, so that nothing overflows; what is lost is below 2^-22 of the row's largest element.
 #pragma once
@@ -24,10 +24,11 @@ struct AdaptersArgs {
     int up_kc;              // up is rank-contiguous (column-major)
     int tiles_m, tiles_n;
     Divisor by_band, by_last_rows;
-    // few rows
     float *t;               // T's slices, [t_slices][rows][t_pitch]
-    float *part;            // the product's, [slices][rows][part_pitch]
-    int t_pitch, t_slices, t_k, turns, part_pitch, slices, k_slice;  // t_k, k_slice: k of a slice
+    int t_pitch, t_slices, t_k, turns;  // t_k: k of a slice; turns: see down_slice
+    // few rows
+    float *part;            // the product's slices, [slices][rows][part_pitch]
+    int part_pitch, slices, k_slice;
     int down_groups;        // workgroups of the launch that compute T
     // many rows
     void *t_parts;          // [rows][parts][t_pitch], t_pitch a multiple of 64
@@ -42,56 +43,6 @@ __device__ __forceinline__ int adapter_at(const AdaptersArgs &p, int row)
 }
 
 constexpr int DOWN_ROWS = 32, DOWN_WAVES = 4;
-typedef float down_part_t[DOWN_WAVES][32][33];
-
-// ---------------------------------------------------------------------------
-// Rows m0 .. m0 + 31 of A times 32 columns of a down matrix, k from k0 to k1: the waves share out the k-groups, and their sums meet in
-// LDS, in wave order.  sum(r, q): row r's element of column q0 + q is handed to `take`.  KC: down is K-contiguous.
-// ---------------------------------------------------------------------------
-template <typename T, bool KC, typename Take>
-__device__ __forceinline__ void down_block(const AdaptersArgs &p, const T *down, int row, int q0, int k0, int k1, down_part_t &part, int tid, int wave, int lane,
-                                           const Take &take)
-{
-    constexpr int KG = Elem<T>::KG, EPL = KG / 2;
-    typedef typename Frag<T>::type frag_t;
-    const int q = q0 + (lane & 31) < p.rank ? q0 + (lane & 31) : p.rank - 1;
-    float16_t acc;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-    // four groups' operands are asked for before the first is multiplied
-    constexpr int AHEAD = 4;
-    int k = k0 + wave * KG;
-    for (; k + (AHEAD - 1) * DOWN_WAVES * KG + KG <= k1; k += AHEAD * DOWN_WAVES * KG) {
-        frag_t fa[AHEAD], fb[AHEAD];
-#pragma unroll
-        for (int x = 0; x < AHEAD; ++x) {
-            const int kl = k + x * DOWN_WAVES * KG + (lane >> 5) * EPL;
-            fa[x] = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, true);
-            fb[x] = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, true);
-        }
-#pragma unroll
-        for (int x = 0; x < AHEAD; ++x) mma(acc, fa[x], fb[x]);
-    }
-    for (; k < k1; k += DOWN_WAVES * KG) {
-        const int kl = k + (lane >> 5) * EPL;
-        const bool full = k + KG <= p.K;
-        const frag_t fa = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, full);
-        const frag_t fb = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, full);
-        mma(acc, fa, fb);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) part[wave][8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)][lane & 31] = acc[r];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = i * 8 + (tid >> 5);
-        float sum = part[0][r][tid & 31];
-#pragma unroll
-        for (int w = 1; w < DOWN_WAVES; ++w) sum += part[w][r][tid & 31];
-        take(r, tid & 31, sum);
-    }
-    __syncthreads();
-}
 
 // the next higher adapter number of the wave's lanes whose remainder is `turn`; 0xffffffff if there is none
 __device__ __forceinline__ uint32_t next_adapter(int id, int above, uint32_t turn, uint32_t turns)
@@ -100,13 +51,16 @@ __device__ __forceinline__ uint32_t next_adapter(int id, int above, uint32_t tur
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: slices of T.  Workgroup `item` of down_groups: 32 rows, a slice of K, and of the adapters that the rows have those whose
-// number is its turn's.
+// Slices of T straight from memory to the matrix instructions, any alignment: a wave takes 32 rows, a slice of K, and of the adapters that
+// the rows have those whose number is its turn's.  Wave `item` of row tiles x slices x turns.  KC: down is K-contiguous.
 // ---------------------------------------------------------------------------
-template <typename T, bool KC> __device__ __forceinline__ void down_slice(const AdaptersArgs &p, int item, down_part_t &part, int tid, int wave, int lane)
+template <typename T, bool KC> __device__ __forceinline__ void down_slice(const AdaptersArgs &p, int item, int lane)
 {
+    constexpr int KG = Elem<T>::KG, EPL = KG / 2, AHEAD = 8;
+    typedef typename Frag<T>::type frag_t;
     const uint32_t turn = (uint32_t)item % (uint32_t)p.turns;
     const int rest = item / p.turns, slice = rest % p.t_slices, m0 = rest / p.t_slices * DOWN_ROWS;
+    if (m0 >= p.rows) return;
     const int k0 = slice * p.t_k, k1 = k0 + p.t_k < p.K ? k0 + p.t_k : p.K;
     const int id = adapter_at(p, m0 + (lane & 31));
     const int row = m0 + (lane & 31) < p.rows ? m0 + (lane & 31) : p.rows - 1;
@@ -117,10 +71,38 @@ template <typename T, bool KC> __device__ __forceinline__ void down_slice(const 
         a = __builtin_amdgcn_readfirstlane((int)next);
         const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
         const T *const down = (const T *)p.down + (int64_t)a * p.stride_down;
-        for (int q0 = 0; q0 < p.rank; q0 += 32)
-            down_block<T, KC>(p, down, row, q0, k0, k1, part, tid, wave, lane, [&](int r, int q, float sum) {
-                if (q0 + q < p.rank && adapter_at(p, m0 + r) == a) p.t[((int64_t)slice * p.rows + m0 + r) * p.t_pitch + q0 + q] = scale * sum;
-            });
+        for (int q0 = 0; q0 < p.rank; q0 += 32) {
+            const int q = q0 + (lane & 31) < p.rank ? q0 + (lane & 31) : p.rank - 1;
+            float16_t acc;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+            // the operands of eight k-groups are asked for before the first is multiplied
+            int k = k0;
+            for (; k + AHEAD * KG <= k1; k += AHEAD * KG) {
+                frag_t fa[AHEAD], fb[AHEAD];
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) {
+                    const int kl = k + x * KG + (lane >> 5) * EPL;
+                    fa[x] = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, true);
+                    fb[x] = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, true);
+                }
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) mma(acc, fa[x], fb[x]);
+            }
+            for (; k < k1; k += KG) {
+                const int kl = k + (lane >> 5) * EPL;
+                const bool full = k + KG <= p.K;
+                const frag_t fa = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, full);
+                const frag_t fb = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, full);
+                mma(acc, fa, fb);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int x = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+                const int of = __shfl(id, x);  // (by all lanes)
+                if (of == a && q0 + (lane & 31) < p.rank) p.t[((int64_t)slice * p.rows + m0 + x) * p.t_pitch + q0 + (lane & 31)] = scale * acc[r];
+            }
+        }
     }
 }
 
@@ -132,14 +114,13 @@ __global__ __launch_bounds__(256) void adapters_slices_kernel(const AdaptersArgs
 {
     typedef TileLoop<T, BM, BN, BM / 32, 4 / (BM / 32), NST, true, BKC> Loop;
     constexpr int WM = BM / 32, WN = 4 / WM;
-    union Lds { char stages[Loop::LDS_BYTES]; down_part_t part; };
-    __shared__ __attribute__((aligned(1024))) Lds smem;
+    __shared__ __attribute__((aligned(1024))) char smem[Loop::LDS_BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if ((int)blockIdx.x < p.down_groups) {
-        down_slice<T, DKC>(p, blockIdx.x, smem.part, tid, wave, lane);
+    if ((int)blockIdx.x < p.down_groups) {  // (first: they wait for memory while the others stream)
+        down_slice<T, DKC>(p, (int)blockIdx.x * DOWN_WAVES + wave, lane);
         return;
     }
-    GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem.stages;
+    GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
     // slices of a tile are neighbours, tiles of one column of them follow each other
     const int item = (int)blockIdx.x - p.down_groups, slice = item % p.slices, tile = item / p.slices;
     const int tile_n = tile / p.tiles_m, tile_m = tile - tile_n * p.tiles_m;
@@ -175,24 +156,35 @@ __global__ __launch_bounds__(256) void adapters_slices_kernel(const AdaptersArgs
 // ---------------------------------------------------------------------------
 // Few rows: C from the slices.  A workgroup takes one row and JOIN_COLS columns; T's row waits in LDS, every thread has four columns.
 // ---------------------------------------------------------------------------
-constexpr int JOIN_COLS = 1024;
+constexpr int JOIN_COLS = 1024, JOIN_T = 4096;  // columns of a workgroup, elements of T's slices that it holds
 template <typename T, typename TC> __global__ __launch_bounds__(256) void adapters_join_kernel(const AdaptersArgs p)
 {
     constexpr int EPC = Elem<T>::EPC;
     typedef T vec_t __attribute__((ext_vector_type(EPC)));
     typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
-    __shared__ float t[256];
+    __shared__ float t[256], t_part[JOIN_T];
     const int row = blockIdx.x, tid = threadIdx.x;
     const int col = (int)blockIdx.y * JOIN_COLS + tid * 4;
     const int a = adapter_at(p, row);
-    if (a >= 0 && tid < p.rank) {
-        float sum = p.t[(int64_t)row * p.t_pitch + tid];
-        for (int s = 1; s < p.t_slices; ++s) sum += p.t[((int64_t)s * p.rows + row) * p.t_pitch + tid];
-        t[tid] = sum;
-    }
+    // (everything is asked for at once: a load after the other costs a memory round trip each)
     float4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (col < p.N) {  // (a row of slices is padded to whole pieces)
-        for (int s = 0; s < p.slices; ++s) acc += *(const float4_t *)(p.part + ((int64_t)s * p.rows + row) * p.part_pitch + col);
+    const float *part = p.part + (int64_t)row * p.part_pitch + (col < p.N ? col : 0);  // (a row of slices is padded to whole pieces)
+    const int64_t slice = (int64_t)p.rows * p.part_pitch;
+    constexpr int AHEAD = 8;
+    for (int s0 = 0; s0 < p.slices; s0 += AHEAD) {
+        float4_t v[AHEAD];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) v[s] = s0 + s < p.slices ? *(const float4_t *)(part + (s0 + s) * slice) : float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (s0 == 0 && a >= 0)
+            for (int x = tid; x < p.t_slices * p.rank; x += 256) t_part[x] = p.t[((int64_t)(x / p.rank) * p.rows + row) * p.t_pitch + x % p.rank];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) acc += v[s];
+    }
+    __syncthreads();
+    if (a >= 0 && tid < p.rank) {
+        float sum = t_part[tid];
+        for (int s = 1; s < p.t_slices; ++s) sum += t_part[s * p.rank + tid];
+        t[tid] = sum;
     }
     __syncthreads();
     if (col >= p.N) return;
@@ -232,38 +224,57 @@ template <> struct Parts<_Float16> { static constexpr int N = 2; };
 template <> struct Parts<__bf16> { static constexpr int N = 3; };  // (with binary32's exponents: needs no scaling)
 
 // ---------------------------------------------------------------------------
-// Many rows: the rows of adapter a among m0 .. m0 + 31 of T, full in LDS, to parts.  Eight neighbouring threads have a row.
+// Many rows: T's slices added up, in slice order, and cut into parts.  Eight neighbouring threads have a row.
 // ---------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ void store_parts(const AdaptersArgs &p, const float *full, int pitch, int m0, int a, int tid)
+template <typename T> __global__ __launch_bounds__(256) void adapters_parts_kernel(const AdaptersArgs p)
 {
     constexpr int NP = Parts<T>::N;
-    const int r = tid / 8, g = tid % 8;
-    const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
-    const bool mine = adapter_at(p, m0 + r) == a;
+    const int row = (int)blockIdx.x * 32 + (int)threadIdx.x / 8, g = threadIdx.x % 8;
+    const bool mine = adapter_at(p, row) >= 0;
+    auto pieces = [&](int q0, float (&v)[8]) {  // T's elements q0 .. q0 + 7 (pitch and slices are whole pieces)
+        const float *t = p.t + (int64_t)row * p.t_pitch + q0;
+        float4_t lo = *(const float4_t *)t, hi = *(const float4_t *)(t + 4);
+#pragma unroll 4
+        for (int s = 1; s < p.t_slices; ++s) {
+            t += (int64_t)p.rows * p.t_pitch;
+            lo += *(const float4_t *)t;
+            hi += *(const float4_t *)(t + 4);
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = q0 + x < p.rank ? (x < 4 ? lo[x & 3] : hi[x & 3]) : 0.0f;
+    };
     float factor = 1.0f;
     if constexpr (std::is_same<T, _Float16>::value) {
         float m = 0.0f;
-        for (int q = g; q < p.rank; q += 8) m = fmaxf(m, fabsf(scale * full[r * pitch + q]));
+        if (mine)
+            for (int q0 = g * 8; q0 < p.rank; q0 += 64) {
+                float v[8];
+                pieces(q0, v);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) m = fmaxf(m, fabsf(v[x]));
+            }
 #pragma unroll
         for (int s = 1; s < 8; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
         int e = 0;
         if (m > 0.0f && m < INFINITY) e = ilogbf(m);
         e = e < -126 ? -126 : e;  // (2^-e has to be a number)
         factor = ldexpf(1.0f, -e);
-        if (mine && g == 0) p.t_scale[m0 + r] = ldexpf(1.0f, e);
+        if (mine && g == 0) p.t_scale[row] = ldexpf(1.0f, e);
     }
     if (!mine) return;
-    T *const out = (T *)p.t_parts + (int64_t)(m0 + r) * NP * p.t_pitch;
+    T *const out = (T *)p.t_parts + (int64_t)row * NP * p.t_pitch;
     for (int q0 = g * 8; q0 < p.t_pitch; q0 += 64) {
+        float left[8];
+        if (q0 < p.rank) pieces(q0, left);
         T v[NP][8];
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-            float left = q0 + x < p.rank ? scale * full[r * pitch + q0 + x] * factor : 0.0f;
+            float l = q0 < p.rank ? left[x] * factor : 0.0f;
 #pragma unroll
             for (int n = 0; n < NP; ++n) {
-                v[n][x] = rounded<T>(left);
+                v[n][x] = rounded<T>(l);
                 const float part = (float)v[n][x];
-                left = fabsf(part) < INFINITY ? left - part : 0.0f;
+                l = fabsf(part) < INFINITY ? l - part : 0.0f;
             }
         }
 #pragma unroll
@@ -274,47 +285,34 @@ template <typename T> __device__ __forceinline__ void store_parts(const Adapters
     }
 }
 
-// T of 32 rows, any alignment of down
+// T's slices, any alignment of down
 template <typename T, bool KC> __global__ __launch_bounds__(DOWN_WAVES * 64) void adapters_down_any_kernel(const AdaptersArgs p)
 {
-    __shared__ down_part_t part;
-    __shared__ float full[DOWN_ROWS * 257];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m0 = (int)blockIdx.x * DOWN_ROWS;
-    const int id = adapter_at(p, m0 + (lane & 31));
-    const int row = m0 + (lane & 31) < p.rows ? m0 + (lane & 31) : p.rows - 1;
-    int a = -1;
-    for (;;) {
-        const uint32_t next = next_adapter(id, a, 0, 1);
-        if (next == 0xffffffffu) break;
-        a = __builtin_amdgcn_readfirstlane((int)next);
-        const T *const down = (const T *)p.down + (int64_t)a * p.stride_down;
-        for (int q0 = 0; q0 < p.rank; q0 += 32)
-            down_block<T, KC>(p, down, row, q0, 0, p.K, part, tid, wave, lane, [&](int r, int q, float sum) { full[r * 257 + q0 + q] = sum; });
-        store_parts<T>(p, full, 257, m0, a, tid);
-        __syncthreads();
-    }
+    down_slice<T, KC>(p, (int)blockIdx.x * DOWN_WAVES + wave, lane);
 }
 
 // ---------------------------------------------------------------------------
-// T of 32 rows on direct loads: BN columns at once (rank, rounded up), NST stages of 64 k; every wave multiplies one k-group of a slab, so that
-// a fragment is read from LDS once, and the waves' sums meet in LDS, in wave order.
+// T's slices on direct loads: BM rows and BN columns (rank, rounded up) at once, NST stages of 64 k; every wave multiplies one k-group of a
+// slab, so that a fragment is read from LDS once, and the waves' sums meet in LDS, in wave order.  What bounds it is
+// how much is on its way: 32 rows of the whole K took 58 us at 8192 x 4096 and rank 64, 64 rows in slices of K take 26.
 // ---------------------------------------------------------------------------
-template <typename T, int BN, int NST, bool KC> __global__ __launch_bounds__(256) void adapters_down_kernel(const AdaptersArgs p)
+template <typename T, int BM, int BN, int NST, bool KC> __global__ __launch_bounds__(256) void adapters_down_kernel(const AdaptersArgs p)
 {
-    typedef TileLoop<T, 32, BN, 1, 4, NST, true, KC> Loads;   // (its loaders and images; the multiplication is here)
-    constexpr int BK = Elem<T>::BK, KG = Elem<T>::KG, EPC = Elem<T>::EPC, FN = BN / 32;
+    typedef TileLoop<T, BM, BN, 1, 4, NST, true, KC> Loads;   // (its loaders and images; the multiplication is here)
+    constexpr int BK = Elem<T>::BK, KG = Elem<T>::KG, EPC = Elem<T>::EPC, FM = BM / 32, FN = BN / 32;
     typedef typename Frag<T>::type frag_t;
-    constexpr int PITCH = BN + 1;
-    constexpr int SUMS = 32 * PITCH * 4 * 4, BYTES = Loads::LDS_BYTES > SUMS ? Loads::LDS_BYTES : SUMS;
+    constexpr int PITCH = BN + 1, SUMS = 32 * PITCH * 4 * 4;  // of 32 rows
+    constexpr int BYTES = Loads::LDS_BYTES > SUMS ? Loads::LDS_BYTES : SUMS;
     static_assert(KGS == 4, "a k-group for each of four waves");
     __shared__ __attribute__((aligned(1024))) char smem[BYTES];
     GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
     float *const sums = (float *)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m0 = (int)blockIdx.x * DOWN_ROWS;
-    const int id = adapter_at(p, m0 + (lane & 31));
-    const int n = (p.K + BK - 1) / BK, krem = p.K - (n - 1) * BK;
+    const int slice = (int)blockIdx.x % p.t_slices, m0 = (int)blockIdx.x / p.t_slices * BM;
+    const int k0 = slice * p.t_k, k1 = k0 + p.t_k < p.K ? k0 + p.t_k : p.K;
+    const int id = lane < BM ? adapter_at(p, m0 + lane) : -1;
+    const int n = (k1 - k0 + BK - 1) / BK, krem = k1 - k0 - (n - 1) * BK;
     int a = -1;
     for (;;) {
         const uint32_t next = next_adapter(id, a, 0, 1);
@@ -322,8 +320,8 @@ template <typename T, int BN, int NST, bool KC> __global__ __launch_bounds__(256
         a = __builtin_amdgcn_readfirstlane((int)next);
         typename Loads::LoaderA la;
         typename Loads::LoaderB lb;
-        la.init((const T *)p.A, p.lda, m0, p.rows, p.K, 0, wave, lane);
-        lb.init((const T *)p.down + (int64_t)a * p.stride_down, p.ld_down, 0, p.rank, p.K, 0, wave, lane);
+        la.init((const T *)p.A, p.lda, m0, p.rows, p.K, k0, wave, lane);
+        lb.init((const T *)p.down + (int64_t)a * p.stride_down, p.ld_down, 0, p.rank, p.K, k0, wave, lane);
         auto at = [&](int h) {
             if (h > 0) {
                 la.advance();
@@ -336,11 +334,13 @@ template <typename T, int BN, int NST, bool KC> __global__ __launch_bounds__(256
                 lb.ragged_slab(krem, wave, lane);
             }
         };
-        float16_t acc[FN];
+        float16_t acc[FM][FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[j][r] = 0.0f;
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
         const int part = krem % EPC, half = krem % KG / EPC;
         auto multiply = [&](const GEMM_LDS(char) * sA, const GEMM_LDS(char) * sB, bool last) {
             if (last && wave * KG >= krem) return;
@@ -352,39 +352,46 @@ template <typename T, int BN, int NST, bool KC> __global__ __launch_bounds__(256
                     mask[w] = in >= 4 ? 0xffffffffu : (in == 2 ? 0x0000ffffu : 0u);
                 }
             }
-            const frag_t fa = __builtin_bit_cast(frag_t, __builtin_bit_cast(uint4_t, fetch_group<T, 32, true>(sA, 0, wave, lane)) & mask);
-            frag_t fb[FN];
+            frag_t fa[FM], fb[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+                fa[i] = __builtin_bit_cast(frag_t, __builtin_bit_cast(uint4_t, fetch_group<T, BM, true>(sA, i * 32, wave, lane)) & mask);
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 fb[j] = fetch_group<T, BN, KC>(sB, j * 32, wave, lane);
                 if (KC) fb[j] = __builtin_bit_cast(frag_t, __builtin_bit_cast(uint4_t, fb[j]) & mask);
             }
 #pragma unroll
-            for (int j = 0; j < FN; ++j) mma(acc[j], fa, fb[j]);
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) mma(acc[i][j], fa[i], fb[j]);
         };
         Loads::run_with(la, lb, at, n, lds, wave, multiply);
-        __syncthreads();
+        const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int i = 0; i < FM; ++i) {
+            __syncthreads();  // every wave has read its last operands, or the sums before
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sums[(wave * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * PITCH + j * 32 + (lane & 31)] = acc[j][r];
-        __syncthreads();
-        for (int x = tid; x < 32 * BN; x += 256) {
-            const int r = x / BN, q = x % BN;
-            float s = sums[r * PITCH + q];
+            for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int w = 1; w < 4; ++w) s += sums[(w * 32 + r) * PITCH + q];
-            sums[r * PITCH + q] = s;  // (only this thread reads or writes it)
+                for (int r = 0; r < 16; ++r) sums[(wave * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * PITCH + j * 32 + (lane & 31)] = acc[i][j][r];
+            __syncthreads();
+            for (int x = tid; x < 32 * BN; x += 256) {
+                const int r = x / BN, q = x % BN, row = m0 + i * 32 + r;
+                float s = sums[r * PITCH + q];
+#pragma unroll
+                for (int w = 1; w < 4; ++w) s += sums[(w * 32 + r) * PITCH + q];
+                const int of = __shfl(id, i * 32 + r);  // (by all lanes)
+                if (of == a && q < p.rank) p.t[((int64_t)slice * p.rows + row) * p.t_pitch + q] = scale * s;
+            }
         }
-        __syncthreads();
-        store_parts<T>(p, sums, PITCH, m0, a, tid);
         __syncthreads();
     }
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: the additions of a tile and its store, 32 rows of every wave at a time (a band): the band's accumulators leave the accumulation
-// registers, which makes room for the additions', and go out as in store_rows.  lds: the K loop's, drained of loads.
+// Many rows: the additions of a tile and its store, 32 rows of every row of waves at a time, neighbours (a band: few adapters): its accumulators
+// leave the accumulation registers, which makes room for the additions', and go out as in store_rows.  lds: the K loop's, drained of loads.
 // Rows of other adapters take part in a product and are not taken over: masked to zeros they would meet the adapter's matrix
 // all the same, and a NaN or an infinity in it would reach them.
 // ---------------------------------------------------------------------------
@@ -397,14 +404,36 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
     constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     constexpr int BAND = WM * 32, T_BYTES = BAND * RBK, U_BYTES = BN * RBK;  // images of a band of T, of an up matrix
     constexpr int SW = TN + 8, EL = 16 / (int)sizeof(TC), LPR = TN / EL, RPI = 64 / LPR;
-    constexpr int AT_T = U_BYTES, AT_IDS = AT_T + NP * T_BYTES, AT_STAGE = AT_IDS + BM * 8;
-    static_assert(AT_STAGE + WM * WN * 32 * SW * 4 <= LDS_BYTES, "images and staging area");
+    constexpr int STAGES = WM * WN * 32 * SW * 4;
+    // up matrices of two adapters where there is room: with runs of rows longer than a tile there are no more
+    constexpr int NU = 2 * U_BYTES + NP * T_BYTES + BM * 8 + STAGES <= LDS_BYTES ? 2 : 1;
+    constexpr int AT_T = NU * U_BYTES, AT_IDS = AT_T + NP * T_BYTES, AT_STAGE = AT_IDS + BM * 8;
+    static_assert(AT_STAGE + STAGES <= LDS_BYTES, "images and staging area");
     typedef TC vec_t __attribute__((ext_vector_type(EL)));
     typedef vec_t loose_t __attribute__((aligned(sizeof(TC))));
     GEMM_LDS(int) *ids = (GEMM_LDS(int) *)(lds + AT_IDS);
     GEMM_LDS(float) *scale = (GEMM_LDS(float) *)(lds + AT_IDS + BM * 4);
     GEMM_LDS(float) *stage = (GEMM_LDS(float) *)(lds + AT_STAGE + wave * (32 * SW * 4));
     const int wm = wave / WN, wn = wave % WN, rows = p.rows - m0, cols = p.N - n0;
+    // T's rows of a band: whole granules, one row of threads for each of the parts
+    auto stage_t = [&](int band, int q0) {
+        constexpr int ITERS = BAND * GPR / NT;
+        uint4_t v[NP][ITERS];
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const int x = (tid + i * NT) / GPR, g = tid % GPR, row = m0 + band * BAND + x;
+            const T *const t = (const T *)p.t_parts + (int64_t)(row < p.rows ? row : p.rows - 1) * NP * p.t_pitch + q0 + g * Elem<T>::EPC;
+#pragma unroll
+            for (int n = 0; n < NP; ++n) v[n][i] = *(const uint4_t *)(t + n * p.t_pitch);
+        }
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const int x = (tid + i * NT) / GPR, g = tid % GPR;
+#pragma unroll
+            for (int n = 0; n < NP; ++n) *(GEMM_LDS(uint4_t) *)(lds + AT_T + n * T_BYTES + x * RBK + ((g ^ swz_kc(x)) << 4)) = v[n][i];
+        }
+    };
+    const bool at_once = p.rank <= BK;  // T's and the up matrices' images hold all of rank
     __syncthreads();  // every wave has read its last operands
     for (int r = tid; r < BM; r += NT) {
         const int a = adapter_at(p, m0 + r);
@@ -412,54 +441,41 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
         scale[r] = std::is_same<T, _Float16>::value && a >= 0 ? p.t_scale[m0 + r] : 1.0f;
     }
     __syncthreads();
-    int staged_a = -1, staged_q = 0;  // what the image of the up matrix holds
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        float16_t band[FN];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            band[j] = acc[i][j];
-            asm volatile("" : "+v"(band[j]));
-        }
-        auto band_row = [&](int x) { return x / 32 * TM + i * 32 + x % 32; };
-        int a = -1;
-        bool t_there = false;
-        for (;;) {
+    int held[2] = {-1, -1}, victim = 0;  // adapters whose up matrices are there (all of rank)
+    auto store_band = [&](auto i_tag, float16_t(&band)[FN]) {
+        constexpr int i = decltype(i_tag)::value;
+        auto next_of = [&](int above) {
             uint32_t next = 0xffffffffu;
             for (int x = lane; x < BAND; x += 64) {
-                const int id = ids[band_row(x)];
-                if (id > a && (uint32_t)id < next) next = (uint32_t)id;
+                const int id = ids[i * BAND + x];
+                if (id > above && (uint32_t)id < next) next = (uint32_t)id;
             }
-            next = umin_over<64>(next);
-            if (next == 0xffffffffu) break;
-            a = __builtin_amdgcn_readfirstlane((int)next);
+            return (int)__builtin_amdgcn_readfirstlane((int)umin_over<64>(next));
+        };
+        int a = p.adapters > 0 ? next_of(-1) : -1;
+        if (at_once && a != -1) stage_t(i, 0);
+        while (a != -1) {
             const T *const up = (const T *)p.up + (int64_t)a * p.stride_up;
             for (int q0 = 0; q0 < p.rank; q0 += BK) {
-                if (!t_there) {
-#pragma unroll 1
-                    for (int n = 0; n < NP; ++n) {
-                        GranuleLoader<T, BAND, NT, true> t;
-                        t.fetch([&](int x) -> const T * {
-                            const int row = m0 + band_row(x);
-                            return row < p.rows ? (const T *)p.t_parts + ((int64_t)row * NP + n) * p.t_pitch : nullptr;
-                        }, 0, p.t_pitch, q0, tid);
-                        t.store(lds + AT_T + n * T_BYTES, tid);
-                    }
-                    t_there = p.rank <= BK;
-                }
-                if (staged_a != a || staged_q != q0) {
+                if (!at_once) stage_t(i, q0);
+                int slot = at_once && held[0] == a ? 0 : (at_once && NU == 2 && held[1] == a ? 1 : -1);
+                if (slot < 0) {
+                    slot = victim;
+                    if (victim == 0) held[0] = a;
+                    else held[1] = a;
+                    victim = NU == 2 ? 1 - victim : 0;
+                    GEMM_LDS(char) *const img = lds + slot * U_BYTES;
                     if (p.up_kc) {
                         GranuleLoader<T, BN, NT, true> u;
                         u.fetch([&](int c) -> const T * { return n0 + c < p.N ? up + (int64_t)(n0 + c) * p.ld_up : nullptr; }, 0, p.rank, q0, tid);
-                        u.store(lds, tid);
+                        u.store(img, tid);
                     } else {
                         GranuleLoader<T, BN, NT, false> u;
                         u.fetch([&](int q) -> const T * { return q < p.rank ? up + (int64_t)q * p.ld_up : nullptr; }, n0, p.N, q0, tid);
-                        u.store(lds, tid);
+                        u.store(img, tid);
                     }
-                    staged_a = a;
-                    staged_q = q0;
                 }
+                const GEMM_LDS(char) *const img = lds + slot * U_BYTES;
                 __syncthreads();
                 float16_t add[FN];
 #pragma unroll
@@ -473,14 +489,14 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
                     for (int n = 0; n < NP; ++n) fa[n] = fetch_group<T, BAND, true>(lds + AT_T + n * T_BYTES, wm * 32, kg, lane);
 #pragma unroll
                     for (int j = 0; j < FN; ++j) {
-                        const frag_t fb = p.up_kc ? fetch_group<T, BN, true>(lds, wn * TN + j * 32, kg, lane) : fetch_group<T, BN, false>(lds, wn * TN + j * 32, kg, lane);
+                        const frag_t fb = p.up_kc ? fetch_group<T, BN, true>(img, wn * TN + j * 32, kg, lane) : fetch_group<T, BN, false>(img, wn * TN + j * 32, kg, lane);
 #pragma unroll
                         for (int n = NP - 1; n >= 0; --n) mma(add[j], fa[n], fb);  // the small parts first
                     }
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int row = wm * TM + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+                    const int row = i * BAND + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
                     const bool mine = ids[row] == a;
                     const float f = scale[row];
 #pragma unroll
@@ -488,6 +504,7 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
                 }
                 __syncthreads();  // the images are done with
             }
+            a = next_of(a);
         }
         // (a wave's staging area is its own)
 #pragma unroll
@@ -497,7 +514,7 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
         const int col = wn * TN + lane % LPR * EL;
 #pragma unroll
         for (int it = 0; it < 32 / RPI; ++it) {
-            const int row = wm * TM + i * 32 + it * RPI + lane / LPR;
+            const int row = i * BAND + wm * 32 + it * RPI + lane / LPR;
             const GEMM_LDS(float) *src = stage + (it * RPI + lane / LPR) * SW + lane % LPR * EL;
             vec_t v;
 #pragma unroll
@@ -513,7 +530,24 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
                     if (col + x < cols) dst[x] = v[x];
             }
         }
+    };
+    // (a band's number has to be a constant, and its accumulators to leave the accumulation registers)
+#define ADAPTERS_BAND(I)                                                                  \
+    if constexpr (I < FM) {                                                               \
+        float16_t band[FN];                                                               \
+        _Pragma("unroll") for (int j = 0; j < FN; ++j)                                    \
+        {                                                                                 \
+            band[j] = acc[I < FM ? I : 0][j];                                             \
+            asm volatile("" : "+v"(band[j]));                                             \
+        }                                                                                 \
+        store_band(std::integral_constant<int, I>(), band);                               \
     }
+    static_assert(FM <= 4, "the bands below");
+    ADAPTERS_BAND(0)
+    ADAPTERS_BAND(1)
+    ADAPTERS_BAND(2)
+    ADAPTERS_BAND(3)
+#undef ADAPTERS_BAND
 }
 
 // tile of this workgroup: every XCD one contiguous run, in bands of tile rows
@@ -528,7 +562,7 @@ __device__ __forceinline__ bool adapters_tile(const AdaptersArgs &p, int &tile_m
 template <typename T, typename TC, int BM, int BN, bool BKC>
 __global__ __launch_bounds__(256) void adapters_ring_kernel(const AdaptersArgs p)
 {
-    typedef RingLoop<T, BM, BN, 2, 2, true, BKC> Loop;
+    typedef RingLoop<T, BM, BN, 2, 2, true, BKC, true> Loop;
     __shared__ __attribute__((aligned(1024))) char smem[Loop::LDS_BYTES];
     GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -197,10 +197,11 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
                 const int64_t row_tiles = ceil_div(rows, DOWN_ROWS);
                 a.turns = (int)std::min<int64_t>(adapters, DOWN_ROWS);
                 a.t_pitch = (int)(ceil_div(rank, 32) * 32);
-                const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(num_cu / std::max<int64_t>(1, row_tiles), ceil_div(K, 256)));
+                // slices of at least 256 k, as many as the second launch holds of a row
+                const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(num_cu / row_tiles, JOIN_T / rank), K / 256));
                 a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
                 a.t_slices = (int)ceil_div(K, a.t_k);
-                a.down_groups = (int)(row_tiles * a.t_slices * a.turns);
+                a.down_groups = (int)ceil_div(row_tiles * a.t_slices * a.turns, DOWN_WAVES);
             }
             const size_t t_bytes = (size_t)a.t_slices * rows * a.t_pitch * sizeof(float);
             const int rc = stream_scratch(s, t_bytes + (size_t)a.slices * rows * a.part_pitch * sizeof(float) + 256, scratch);
@@ -224,17 +225,28 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         if (tiles_m > (1LL << 24) || tiles_n > (1LL << 24) || tiles_m * tiles_n > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
         if (some) {
             const int parts = elem == GEMM_ELEM_F32 ? 1 : (elem == GEMM_ELEM_F16 ? 2 : 3);
-            a.t_pitch = (int)(ceil_div(rank, 64) * 64);
-            const size_t part_bytes = (size_t)rows * parts * a.t_pitch * esz;
-            const int rc = stream_scratch(s, part_bytes + rows * sizeof(float), scratch);
-            if (rc != GEMM_OK) return rc;
-            a.t_parts = scratch.ptr;
-            a.t_scale = (float *)((char *)scratch.ptr + part_bytes);
-            const dim3 grid((unsigned)ceil_div(rows, DOWN_ROWS));
             const bool fast_down = direct(A, lda, 0, esz) && direct(down, ld_down, stride_down, esz);
-            const int sent = elem == GEMM_ELEM_F32   ? launch_adapters_down<float>(dkc, fast_down, grid, s, a)
-                             : elem == GEMM_ELEM_F16 ? launch_adapters_down<_Float16>(dkc, fast_down, grid, s, a)
-                                                     : launch_adapters_down<__bf16>(dkc, fast_down, grid, s, a);
+            const int64_t row_tiles = ceil_div(rows, down_rows(fast_down, a.rank));
+            // two workgroups a CU, in slices of at least 256 k
+            const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(2 * num_cu / row_tiles, K / 256));
+            a.turns = 1;
+            a.t_pitch = (int)(ceil_div(rank, 64) * 64);
+            a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
+            a.t_slices = (int)ceil_div(K, a.t_k);
+            const size_t t_bytes = (size_t)a.t_slices * rows * a.t_pitch * sizeof(float), part_bytes = (size_t)rows * parts * a.t_pitch * esz;
+            const int rc = stream_scratch(s, t_bytes + part_bytes + rows * sizeof(float), scratch);
+            if (rc != GEMM_OK) return rc;
+            a.t = (float *)scratch.ptr;
+            a.t_parts = (char *)scratch.ptr + t_bytes;
+            a.t_scale = (float *)((char *)a.t_parts + part_bytes);
+            const dim3 grid((unsigned)ceil_div(row_tiles * a.t_slices, fast_down ? 1 : DOWN_WAVES)), sums((unsigned)ceil_div(rows, 32));
+            int sent = elem == GEMM_ELEM_F32   ? launch_adapters_down<float>(dkc, fast_down, grid, s, a)
+                       : elem == GEMM_ELEM_F16 ? launch_adapters_down<_Float16>(dkc, fast_down, grid, s, a)
+                                               : launch_adapters_down<__bf16>(dkc, fast_down, grid, s, a);
+            if (sent != GEMM_OK) return sent;
+            sent = elem == GEMM_ELEM_F32   ? launch_adapters_parts<float>(sums, s, a)
+                   : elem == GEMM_ELEM_F16 ? launch_adapters_parts<_Float16>(sums, s, a)
+                                           : launch_adapters_parts<__bf16>(sums, s, a);
             if (sent != GEMM_OK) return sent;
         }
         a.tiles_m = (int)tiles_m;

@@ -72,21 +72,27 @@ template <typename T> int launch_adapters_slices(bool bkc, bool dkc, bool direct
     return launch_slices_form<T, 64, 5>(bkc, dkc, direct, grid, s, a);
 }
 
-// T of many rows
+// T's slices of many rows (down_rows a workgroup), and their sum
+static inline int down_rows(bool direct, int rank) { return direct && rank <= 128 ? 64 : 32; }
 template <typename T, bool KC> static int launch_down_form(bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
 {
     if (!direct) return enqueue(adapters_down_any_kernel<T, KC>, grid, dim3(256), s, a);
-    if (a.rank <= 64) return enqueue(adapters_down_kernel<T, 64, 6, KC>, grid, dim3(256), s, a);
-    if (a.rank <= 128) return enqueue(adapters_down_kernel<T, 128, 4, KC>, grid, dim3(256), s, a);
-    return enqueue(adapters_down_kernel<T, 256, 4, KC>, grid, dim3(256), s, a);
+    if (a.rank <= 64) return enqueue(adapters_down_kernel<T, 64, 64, 5, KC>, grid, dim3(256), s, a);
+    if (a.rank <= 128) return enqueue(adapters_down_kernel<T, 64, 128, 3, KC>, grid, dim3(256), s, a);
+    return enqueue(adapters_down_kernel<T, 32, 256, 4, KC>, grid, dim3(256), s, a);
 }
 template <typename T> int launch_adapters_down(bool kc, bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
 {
     return kc ? launch_down_form<T, true>(direct, grid, s, a) : launch_down_form<T, false>(direct, grid, s, a);
 }
+template <typename T> int launch_adapters_parts(dim3 grid, hipStream_t s, const AdaptersArgs &a)
+{
+    return enqueue(adapters_parts_kernel<T>, grid, dim3(256), s, a);
+}
 
 #define ROUTED_TYPES(PREFIX, T)                                                                                    \
     PREFIX template int launch_adapters_slices<T>(bool, bool, bool, dim3, hipStream_t, const AdaptersArgs &);       \
+    PREFIX template int launch_adapters_parts<T>(dim3, hipStream_t, const AdaptersArgs &);                          \
     PREFIX template int launch_adapters_down<T>(bool, bool, dim3, hipStream_t, const AdaptersArgs &);
 
 #define ROUTED_FORMS(PREFIX, T, TC)                                                                        \

@@ -111,7 +111,9 @@ template <typename T, int R, int NW> struct RingRowsLoader : RingLoader<T, R, NW
     }
 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC> struct RingLoop {
+// BANDS: block i of a wave is the 32 rows (i * WM + its row of waves) * 32 .. of the tile, so that the waves' i-th blocks are neighbours;
+// otherwise a wave's blocks are.
+template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, bool BANDS = false> struct RingLoop {
     static constexpr int NW = WM * WN, NT = NW * 64;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     static constexpr int A_BYTES = BM * RBK, B_BYTES = BN * RBK, SLOT = A_BYTES > B_BYTES ? A_BYTES : B_BYTES, LDS_BYTES = NSLOT * SLOT;
@@ -126,6 +128,7 @@ template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC> struct
                                                float16_t (&acc)[FM][FN], int wave, int lane)
     {
         const int wm = wave / WN, wn = wave % WN;
+        auto row_of = [&](int i) { return BANDS ? (i * WM + wm) * 32 : wm * TM + i * 32; };
         auto pin_acc = [&]() {  // in the accumulation registers at this point
 #pragma unroll
             for (int i = 0; i < FM; ++i)
@@ -159,9 +162,9 @@ template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC> struct
 #pragma unroll
                     for (int f = 0; f < NF; ++f) {
                         if ((f < NB ? f : NB - 1) != m) continue;
-                        if (f == 0) na[0] = Fetch<T, BM, AKC>::get(iA, wm * TM, kg_next, lane);
+                        if (f == 0) na[0] = Fetch<T, BM, AKC>::get(iA, row_of(0), kg_next, lane);
                         else if (f <= FN) nb[f - 1] = Fetch<T, BN, BKC>::get(iB, wn * TN + (f - 1) * 32, kg_next, lane);
-                        else na[f - FN] = Fetch<T, BM, AKC>::get(iA, wm * TM + (f - FN) * 32, kg_next, lane);
+                        else na[f - FN] = Fetch<T, BM, AKC>::get(iA, row_of(f - FN), kg_next, lane);
                     }
                 }
                 if constexpr (NL > 0) {
@@ -216,11 +219,11 @@ template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC> struct
         frag_t fa[2][FM], fb[2][FN];
         {
             const GEMM_LDS(char) *cA = lds + PA * SLOT, *cB = lds + PB * SLOT;
-            fa[0][0] = Fetch<T, BM, AKC>::get(cA, wm * TM, 0, lane);
+            fa[0][0] = Fetch<T, BM, AKC>::get(cA, row_of(0), 0, lane);
 #pragma unroll
             for (int j = 0; j < FN; ++j) fb[0][j] = Fetch<T, BN, BKC>::get(cB, wn * TN + j * 32, 0, lane);
 #pragma unroll
-            for (int i = 1; i < FM; ++i) fa[0][i] = Fetch<T, BM, AKC>::get(cA, wm * TM + i * 32, 0, lane);
+            for (int i = 1; i < FM; ++i) fa[0][i] = Fetch<T, BM, AKC>::get(cA, row_of(i), 0, lane);
         }
         auto slab_kgroups = [&](const GEMM_LDS(char) * cA, const GEMM_LDS(char) * cB, const GEMM_LDS(char) * nA, const GEMM_LDS(char) * nB, auto load_x_lo,
                                 auto load_x_hi, auto load_y, const bool more, auto near_end, const int h) {
