@@ -13,7 +13,10 @@
  * layouts are GEMM_ROW_MAJOR or GEMM_COL_MAJOR; matrices need element alignment only (multiples of 4 bytes of
  * base, leading dimension and stride are faster, of 16 bytes fastest); int32 and float arrays 4 bytes; work is
  * enqueued on hip_stream, nothing synchronises with the host, and a call that returns a negative status for its
- * arguments has enqueued nothing.  Outputs must not overlap inputs.  All sums are held in binary32, and results do
+ * arguments has enqueued nothing.  gemm_route_plan of many entries, gemm_adapters, and long products of 16-bit operands
+ * that are only 2-byte aligned (which are copied first, half a gigabyte at most) use the stream's workspace; while a
+ * stream is being captured it cannot grow: the first two return GEMM_ERR_WORKSPACE then (make the call once outside the
+ * capture), the copies are left out.  Outputs must not overlap inputs.  All sums are held in binary32, and results do
  * not depend on the order in which workgroups run.
  *
  * Device arrays of numbers (expert numbers, offsets, slots, adapter numbers) cannot be checked by the host.  The

@@ -584,7 +584,7 @@ __global__ __launch_bounds__(256) void adapters_ring_kernel(const AdaptersArgs p
 template <typename T, typename TC, int BM, int BN, bool BKC>
 __global__ __launch_bounds__(256) void adapters_any_kernel(const AdaptersArgs p)
 {
-    typedef TileLoop<T, BM, BN, 2, 2, 4, true, BKC> Loop;  // (two stages are used: the rest is room for the additions)
+    typedef TileLoop<T, BM, BN, 2, 2, BM == 64 ? 4 : 3, true, BKC, true> Loop;  // (two stages are used: the rest is room for the additions)
     __shared__ __attribute__((aligned(1024))) char smem[Loop::LDS_BYTES];
     GEMM_LDS(char) *lds = (GEMM_LDS(char) *)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

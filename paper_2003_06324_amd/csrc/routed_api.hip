@@ -49,6 +49,111 @@ int grouped_form(int64_t groups, int64_t rows, int64_t N, int64_t K, int64_t num
     return of256 <= of128 ? GROUPED_256x256 : GROUPED_128x128;
 }
 
+// ---------------------------------------------------------------------------
+// Operands whose rows lie in the middle of 4-byte words are copied to rows of whole cache lines first, where the product is long enough:
+// direct loads cannot serve them, and through registers the memory pipeline splits every 16-byte load.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void pack_rows_kernel(const uint16_t *src, int64_t ld, int64_t stride, uint16_t *dst, int64_t ld_to, int64_t rows, int cols,
+                                                        int per_row, Divisor by_per_row)
+{
+    // (a row of the launch is a matrix; its threads take the granules of its rows one after the other)
+    typedef uint4_t loose_t __attribute__((aligned(2)));
+    src += (int64_t)blockIdx.y * stride;
+    dst += (int64_t)blockIdx.y * rows * ld_to;
+    const int64_t granules = rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < granules; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = granules < (1LL << 28) ? divide((int)i, by_per_row) : i / per_row;
+        const int col = (int)(i - row * per_row) * 8;
+        const uint16_t *from = src + row * ld + col;
+        uint4_t w = {0u, 0u, 0u, 0u};
+        if (col + 8 <= cols) {
+            w = *(const loose_t *)from;
+        } else {
+            uint16_t e[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) e[x] = col + x < cols ? from[x] : 0;
+            __builtin_memcpy(&w, e, 16);
+        }
+        *(uint4_t *)(dst + row * ld_to + col) = w;
+        behind_wide_store();
+    }
+}
+// A 16-bit matrix, or `count` of them, stored as rows x cols: packed to rows of whole lines where that is needed
+struct Packing {
+    const void **base;
+    int64_t *ld, *stride;
+    int64_t count, rows, cols;
+    bool needed() const { return count > 0 && (((uintptr_t)*base | (uintptr_t)(*ld * 2) | (uintptr_t)(count > 1 ? *stride * 2 : 0)) & 3) != 0; }
+    int64_t pitch() const { return ceil_div(cols, 64) * 64; }
+    int64_t bytes() const { return needed() ? count * rows * pitch() * 2 : 0; }
+    // where and how it lay before describe()
+    const uint16_t *src = nullptr;
+    int64_t src_ld = 0, src_stride = 0;
+    // describes it as it will lie at `to`
+    void describe(char *to)
+    {
+        src = (const uint16_t *)*base;
+        src_ld = *ld;
+        src_stride = count > 1 ? *stride : 0;
+        *base = to;
+        *ld = pitch();
+        *stride = rows * pitch();
+    }
+    // copies it there
+    int copy(hipStream_t s) const
+    {
+        if (src == nullptr) return GEMM_OK;
+        const int per_row = (int)ceil_div(cols, 8);
+        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * per_row, 256), std::max<int64_t>(1, 4096 / count)), (unsigned)count);
+        return enqueue(pack_rows_kernel, grid, dim3(256), s, src, src_ld, src_stride, (uint16_t *)const_cast<void *>(*base), pitch(), rows, (int)cols, per_row,
+                       divisor(per_row));
+    }
+};
+// Whether the copies pay: through registers a product of 16-bit operands runs at 260 .. 340 TFLOP/s, on direct loads at 550 and more, and
+// what is copied is read and written once, at 4 TB/s or so (32 matrices of 2047 x 2048, 512 rows each: 404 us through registers, 277
+// copied, 148 where only A is; their gradients 262 and 130; adapters, 4096 rows, 2047 x 2048, 138 and 74).  At most half a gigabyte is.
+bool packing_pays(double flops, int64_t bytes) { return bytes > 0 && bytes <= (1LL << 29) && flops > 2e9 + 260.0 * (double)bytes; }
+
+// Describes the operands that need it as packed, if that pays and there is room for the copies (and for more_bytes, which `more` then
+// points to).  Nothing is enqueued yet: copy() does that.
+template <size_t N> int plan_packing(Packing (&pack)[N], double flops, hipStream_t s, StreamScratch &scratch, int64_t more_bytes = 0, char **more = nullptr)
+{
+    int64_t bytes = 0;
+    for (const Packing &p : pack) bytes += p.count <= 4096 ? p.bytes() : (1LL << 30);
+    if (!packing_pays(flops, bytes)) bytes = 0;
+    if (bytes + more_bytes == 0) return GEMM_OK;
+    int rc = stream_scratch(s, (size_t)(bytes + more_bytes), scratch);
+    if (rc != GEMM_OK && bytes > 0) {  // (it works without the copies)
+        scratch = StreamScratch();
+        bytes = 0;
+        if (more_bytes > 0) rc = stream_scratch(s, (size_t)more_bytes, scratch);
+        else return GEMM_OK;
+    }
+    if (rc != GEMM_OK) return rc;
+    char *at = (char *)scratch.ptr;
+    if (bytes > 0)
+        for (Packing &p : pack) {
+            const int64_t mine = p.bytes();
+            if (mine == 0) continue;
+            p.describe(at);
+            at += mine;
+        }
+    if (more != nullptr) *more = at;
+    return GEMM_OK;
+}
+template <size_t N> int copy_packed(const Packing (&pack)[N], hipStream_t s)
+{
+    for (const Packing &p : pack) {
+        const int rc = p.copy(s);
+        if (rc != GEMM_OK) return rc;
+    }
+    return GEMM_OK;
+}
+
+// Whether the kernels that fetch through registers take tiles of 128 x 128, which ask for half as much, or of 64 x 64 (32 matrices of
+// 2048 x 2047, 512 rows each 404 and 441 us; 128 of 2047 x 1536, 4 rows each 196 and 155).
+bool any_large(int64_t tiles128, int64_t num_cu) { return tiles128 >= num_cu; }
+
 // Tile of the weight gradients, by the rounds that the chip takes (see grouped_form; 32 matrices of 2048 x 1024, 1024 rows each 155 us on
 // 256 x 256, 220 on 128 x 128).
 int wgrad_form(int64_t groups, int64_t M, int64_t N, int64_t num_cu)
@@ -88,19 +193,34 @@ int gemm_grouped(int kind, int64_t groups, const int32_t *offsets, int64_t rows,
     if (groups == 0 || rows == 0 || N == 0) return GEMM_OK;
     if (offsets == nullptr || C == nullptr || (K > 0 && (B == nullptr || (a_rows > 0 && A == nullptr)))) return GEMM_ERR_INVALID_ARG;
     const int64_t esz = elem_size(kind), num_cu = cu_count();
-    int form = GROUPED_ANY;
-    int64_t BM = 64, BN = 64;
-    if (direct(A, lda, 0, esz) && direct(B, ldb, strideB, esz) && (row_map == nullptr || gathers(a_rows, lda, esz))) {
-        form = grouped_form(groups, rows, N, K, num_cu);
-        BM = form == GROUPED_32x128 ? 32 : (form == GROUPED_128x128 ? 128 : 256);
-        BN = form == GROUPED_256x256 ? 256 : 128;
-    }
-    const int64_t tiles_n = ceil_div(N, BN), grid = grouped_grid(groups, rows, BM, tiles_n);
-    if (grid > (1LL << 24) - 1) return GEMM_ERR_UNSUPPORTED;
-    const GroupedArgs a = {A, B, C, offsets, row_map, lda, ldb, ldc, strideB, (int)groups, (int)rows, (int)a_rows, (int)N, (int)K, (int)tiles_n};
-    return by_kind(kind, [&](auto *t, auto *tc) {
-        return launch_grouped<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(form, layoutB == GEMM_COL_MAJOR, dim3((unsigned)grid),
-                                                                                                       (hipStream_t)hip_stream, a);
+    const hipStream_t s = (hipStream_t)hip_stream;
+    return no_throw([&]() -> int {
+        StreamScratch scratch;
+        int64_t none = 0;
+        Packing pack[] = {{&A, &lda, &none, 1, a_rows, K}, {&B, &ldb, &strideB, groups, layoutB == GEMM_ROW_MAJOR ? K : N, layoutB == GEMM_ROW_MAJOR ? N : K}};
+        if (esz == 2 && K > 0 && a_rows > 0 && (row_map == nullptr || gathers(a_rows, pack[0].pitch(), esz))) {
+            const int rc = plan_packing(pack, 2.0 * (double)rows * (double)N * (double)K, s, scratch);
+            if (rc != GEMM_OK) return rc;
+        }
+        int form = GROUPED_ANY;
+        int64_t BM = 64, BN = 64;
+        if (direct(A, lda, 0, esz) && direct(B, ldb, groups > 1 ? strideB : 0, esz) && (row_map == nullptr || gathers(a_rows, lda, esz))) {
+            form = grouped_form(groups, rows, N, K, num_cu);
+            BM = form == GROUPED_32x128 ? 32 : (form == GROUPED_128x128 ? 128 : 256);
+            BN = form == GROUPED_256x256 ? 256 : 128;
+        } else if (rows > 64 * groups && any_large((rows / 128 + (groups + 1) / 2) * ceil_div(N, 128), num_cu)) {
+            form = GROUPED_ANY128;
+            BM = BN = 128;
+        }
+        const int64_t tiles_n = ceil_div(N, BN), grid = grouped_grid(groups, rows, BM, tiles_n);
+        if (grid > (1LL << 24) - 1) return GEMM_ERR_UNSUPPORTED;
+        const int rc = copy_packed(pack, s);
+        if (rc != GEMM_OK) return rc;
+        const GroupedArgs a = {A, B, C, offsets, row_map, lda, ldb, ldc, strideB, (int)groups, (int)rows, (int)a_rows, (int)N, (int)K, (int)tiles_n};
+        return by_kind(kind, [&](auto *t, auto *tc) {
+            return launch_grouped<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(form, layoutB == GEMM_COL_MAJOR, dim3((unsigned)grid), s,
+                                                                                                           a);
+        });
     });
 }
 
@@ -120,29 +240,42 @@ int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t
     if (groups == 0 || M == 0 || N == 0) return GEMM_OK;
     if (offsets == nullptr || C == nullptr || (rows > 0 && (D == nullptr || (a_rows > 0 && A == nullptr)))) return GEMM_ERR_INVALID_ARG;
     const int64_t esz = elem_size(kind);
-    // The kernels write rows of C: a column-major C is the row-major C^T = D^T A.
-    WgradArgs a = {A, D, C, offsets, row_map, nullptr, lda, ldd, ldc, strideC, (int)groups, (int)rows, (int)a_rows, (int)rows, (int)M, (int)N, 0, 0, 0};
-    // C is written once; from 256 rows a group on it pays to keep it from displacing the rows in the L2 (32 matrices of 2048 x 1024 in
-    // binary32, 1024 rows each 198 -> 180 us; 64 rows each 62 -> 69)
-    a.stream = rows >= 256 * groups;
-    if (layoutC == GEMM_COL_MAJOR) {
-        std::swap(a.X, a.Y);
-        std::swap(a.map_x, a.map_y);
-        std::swap(a.ldx, a.ldy);
-        std::swap(a.x_rows, a.y_rows);
-        std::swap(a.M, a.N);
-    }
-    // (without a map and with fewer rows in A than there are, they may end anywhere in a group; a map is read 16 numbers at a time)
-    const bool fast = direct(A, lda, 0, esz) && direct(D, ldd, 0, esz) && (row_map == nullptr ? a_rows >= rows : rows >= 64 && gathers(a_rows, lda, esz));
-    const int form = !fast ? WGRAD_ANY : wgrad_form(groups, M, N, cu_count());
-    const int64_t edge = form == WGRAD_ANY ? 64 : (form == WGRAD_128x128 ? 128 : 256);
-    a.tiles_m = (int)ceil_div(a.M, edge);
-    a.tiles_n = (int)ceil_div(a.N, edge);
-    const int64_t per = (int64_t)a.tiles_m * a.tiles_n;
-    if (per > (1LL << 24) || per * groups > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)wgrad_grid(groups, rows, per));
-    return by_kind(kind, [&](auto *t, auto *tc) {
-        return launch_wgrad<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(form, grid, (hipStream_t)hip_stream, a);
+    const int64_t num_cu = cu_count(), tiles256 = ceil_div(M, 256) * ceil_div(N, 256);
+    if (tiles256 * groups > (1LL << 22)) return GEMM_ERR_UNSUPPORTED;
+    const hipStream_t s = (hipStream_t)hip_stream;
+    return no_throw([&]() -> int {
+        StreamScratch scratch;
+        int64_t none = 0;
+        Packing pack[] = {{&A, &lda, &none, 1, a_rows, M}, {&D, &ldd, &none, 1, rows, N}};
+        if (esz == 2 && rows >= 64 && a_rows > 0 && (row_map == nullptr ? a_rows >= rows : gathers(a_rows, pack[0].pitch(), esz))) {
+            const int rc = plan_packing(pack, 2.0 * (double)rows * (double)M * (double)N, s, scratch);
+            if (rc != GEMM_OK) return rc;
+        }
+        // The kernels write rows of C: a column-major C is the row-major C^T = D^T A.
+        WgradArgs a = {A, D, C, offsets, row_map, nullptr, lda, ldd, ldc, strideC, (int)groups, (int)rows, (int)a_rows, (int)rows, (int)M, (int)N, 0, 0, 0};
+        // C is written once; from 256 rows a group on it pays to keep it from displacing the rows in the L2 (32 matrices of 2048 x 1024 in
+        // binary32, 1024 rows each 198 -> 180 us; 64 rows each 62 -> 69)
+        a.stream = rows >= 256 * groups;
+        if (layoutC == GEMM_COL_MAJOR) {
+            std::swap(a.X, a.Y);
+            std::swap(a.map_x, a.map_y);
+            std::swap(a.ldx, a.ldy);
+            std::swap(a.x_rows, a.y_rows);
+            std::swap(a.M, a.N);
+        }
+        // (without a map and with fewer rows in A than there are, they may end anywhere in a group; a map is read 16 numbers at a time)
+        const bool fast = direct(A, lda, 0, esz) && direct(D, ldd, 0, esz) && (row_map == nullptr ? a_rows >= rows : rows >= 64 && gathers(a_rows, lda, esz));
+        const int form = fast ? wgrad_form(groups, M, N, num_cu) : WGRAD_ANY;
+        const int64_t edge = form == WGRAD_ANY ? 64 : (form == WGRAD_256x256 ? 256 : 128);
+        a.tiles_m = (int)ceil_div(a.M, edge);
+        a.tiles_n = (int)ceil_div(a.N, edge);
+        const int64_t grid = wgrad_grid(groups, rows, (int64_t)a.tiles_m * a.tiles_n);
+        if (grid > (1LL << 24) - 1) return GEMM_ERR_UNSUPPORTED;
+        const int rc = copy_packed(pack, s);
+        if (rc != GEMM_OK) return rc;
+        return by_kind(kind, [&](auto *t, auto *tc) {
+            return launch_wgrad<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(form, dim3((unsigned)grid), s, a);
+        });
     });
 }
 
@@ -173,6 +306,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         const int64_t esz = elem_size(kind);
         const int elem = elem_of_kind(kind);
         const bool bkc = layoutB == GEMM_COL_MAJOR, dkc = layout_down == GEMM_COL_MAJOR;
+        int64_t none = 0;
         AdaptersArgs a = {};
         a.A = A, a.B = B, a.down = down, a.up = up, a.C = C, a.adapter_of = adapter_of, a.scales = scales;
         a.lda = lda, a.ldb = ldb, a.ldc = ldc, a.ld_down = ld_down, a.stride_down = stride_down, a.ld_up = ld_up, a.stride_up = stride_up;
@@ -185,11 +319,12 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         const int64_t num_cu = scratch.num_cu;
         scratch.lock.unlock();
         if (ceil_div(rows, 128) * ceil_div(N, 128) < num_cu / 2 && rows <= 65535) {
-            // few rows: tiles of 64 x 64, K in slices of at least 256 k while there are less than two workgroups a CU
+            // few rows: tiles of 64 x 64, K in slices of at least 512 k, one workgroup a CU (64 rows, 4096 x 4096: 4 slices 17.4 us, 2 and 8
+            // 20.4; 256 rows: 2 slices 45, 1 54)
             a.tiles_m = (int)ceil_div(rows, 64);
             a.tiles_n = (int)ceil_div(N, 64);
             const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
-            const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(2 * num_cu / tiles, K / 256));
+            const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(2, num_cu / tiles), K / 512));
             a.k_slice = (int)std::max<int64_t>(64, ceil_div(ceil_div(K, slices), 64) * 64);
             a.slices = (int)ceil_div(K, a.k_slice);
             a.part_pitch = (int)(ceil_div(N, 32) * 32);
@@ -219,26 +354,38 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
                 return launch_adapters_join<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(tc)>>(join, s, a);
             });
         }
-        const int form = !fast ? ADAPTERS_ANY : (ceil_div(rows, 256) * ceil_div(N, 256) < num_cu ? ADAPTERS_128x128 : ADAPTERS_256x256);
-        const int64_t edge = form == ADAPTERS_ANY ? 64 : (form == ADAPTERS_128x128 ? 128 : 256);
+        // many rows
+        const int parts = elem == GEMM_ELEM_F32 ? 1 : (elem == GEMM_ELEM_F16 ? 2 : 3);
+        a.t_pitch = (int)(ceil_div(rank, 64) * 64);
+        // two workgroups a CU for T, in slices of at least 256 k
+        const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(2 * num_cu / ceil_div(rows, rank <= 128 ? 64 : 32), K / 256));
+        a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
+        a.t_slices = (int)ceil_div(K, a.t_k > 0 ? a.t_k : 1);
+        a.turns = 1;
+        const int64_t t_bytes = (int64_t)a.t_slices * rows * a.t_pitch * (int64_t)sizeof(float), part_bytes = rows * parts * a.t_pitch * esz;
+        const int64_t scale_bytes = ceil_div(rows, 64) * 256;
+        Packing pack[] = {{&A, &lda, &none, 1, rows, K}, {&B, &ldb, &none, 1, bkc ? N : K, bkc ? K : N},
+                          {&down, &ld_down, &stride_down, some ? adapters : 0, dkc ? rank : K, dkc ? K : rank}};
+        char *at = nullptr;
+        if (esz == 2 || some) {
+            const int rc = plan_packing(pack, esz == 2 ? 2.0 * (double)rows * (double)N * (double)K : 0.0, s, scratch, some ? t_bytes + part_bytes + scale_bytes : 0, &at);
+            if (rc != GEMM_OK) return rc;
+        }
+        a.A = A, a.B = B, a.down = down, a.lda = lda, a.ldb = ldb, a.ld_down = ld_down, a.stride_down = stride_down;
+        const bool fast_now = direct(A, lda, 0, esz) && direct(B, ldb, 0, esz);
+        const int form = fast_now ? (ceil_div(rows, 256) * ceil_div(N, 256) < num_cu ? ADAPTERS_128x128 : ADAPTERS_256x256)
+                                  : (any_large(ceil_div(rows, 128) * ceil_div(N, 128), num_cu) ? ADAPTERS_ANY128 : ADAPTERS_ANY);
+        const int64_t edge = form == ADAPTERS_ANY ? 64 : (form == ADAPTERS_256x256 ? 256 : 128);
         const int64_t tiles_m = ceil_div(rows, edge), tiles_n = ceil_div(N, edge);
         if (tiles_m > (1LL << 24) || tiles_n > (1LL << 24) || tiles_m * tiles_n > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
+        const int copied = copy_packed(pack, s);
+        if (copied != GEMM_OK) return copied;
         if (some) {
-            const int parts = elem == GEMM_ELEM_F32 ? 1 : (elem == GEMM_ELEM_F16 ? 2 : 3);
-            const bool fast_down = direct(A, lda, 0, esz) && direct(down, ld_down, stride_down, esz);
+            const bool fast_down = direct(A, lda, 0, esz) && direct(down, ld_down, adapters > 1 ? stride_down : 0, esz);
             const int64_t row_tiles = ceil_div(rows, down_rows(fast_down, a.rank));
-            // two workgroups a CU, in slices of at least 256 k
-            const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(2 * num_cu / row_tiles, K / 256));
-            a.turns = 1;
-            a.t_pitch = (int)(ceil_div(rank, 64) * 64);
-            a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
-            a.t_slices = (int)ceil_div(K, a.t_k);
-            const size_t t_bytes = (size_t)a.t_slices * rows * a.t_pitch * sizeof(float), part_bytes = (size_t)rows * parts * a.t_pitch * esz;
-            const int rc = stream_scratch(s, t_bytes + part_bytes + rows * sizeof(float), scratch);
-            if (rc != GEMM_OK) return rc;
-            a.t = (float *)scratch.ptr;
-            a.t_parts = (char *)scratch.ptr + t_bytes;
-            a.t_scale = (float *)((char *)a.t_parts + part_bytes);
+            a.t = (float *)at;
+            a.t_parts = at + t_bytes;
+            a.t_scale = (float *)(at + t_bytes + part_bytes);
             const dim3 grid((unsigned)ceil_div(row_tiles * a.t_slices, fast_down ? 1 : DOWN_WAVES)), sums((unsigned)ceil_div(rows, 32));
             int sent = elem == GEMM_ELEM_F32   ? launch_adapters_down<float>(dkc, fast_down, grid, s, a)
                        : elem == GEMM_ELEM_F16 ? launch_adapters_down<_Float16>(dkc, fast_down, grid, s, a)

@@ -6,8 +6,8 @@
 
 namespace gemm_gfx950 {
 
-// forms of grouped_kernel: rows and columns of a tile; 0: through registers
-enum { GROUPED_ANY = 0, GROUPED_32x128 = 1, GROUPED_128x128 = 2, GROUPED_256x256 = 3 };
+// forms of the experts' products: rows and columns of a tile; ANY, ANY128: through registers, 64 x 64 and 128 x 128
+enum { GROUPED_ANY = 0, GROUPED_32x128 = 1, GROUPED_128x128 = 2, GROUPED_256x256 = 3, GROUPED_ANY128 = 4 };
 
 template <typename T, typename TC, bool BKC> static int launch_grouped_form(int form, dim3 grid, hipStream_t s, const GroupedArgs &a)
 {
@@ -15,6 +15,7 @@ template <typename T, typename TC, bool BKC> static int launch_grouped_form(int 
     case GROUPED_32x128: return enqueue(grouped_kernel<T, TC, 32, 128, 1, 4, 4, BKC>, grid, dim3(256), s, a);
     case GROUPED_128x128: return enqueue(grouped_ring_kernel<T, TC, 128, 128, BKC>, grid, dim3(256), s, a);
     case GROUPED_256x256: return enqueue(grouped_ring_kernel<T, TC, 256, 256, BKC>, grid, dim3(256), s, a);
+    case GROUPED_ANY128: return enqueue(grouped_any_kernel<T, TC, 128, 128, BKC>, grid, dim3(256), s, a);
     default: return enqueue(grouped_any_kernel<T, TC, 64, 64, BKC>, grid, dim3(256), s, a);
     }
 }
@@ -38,12 +39,13 @@ template <typename T, typename TC> int launch_wgrad(int form, dim3 grid, hipStre
 }
 
 // forms of the product of many rows
-enum { ADAPTERS_ANY = 0, ADAPTERS_128x128 = 1, ADAPTERS_256x256 = 2 };
+enum { ADAPTERS_ANY = 0, ADAPTERS_128x128 = 1, ADAPTERS_256x256 = 2, ADAPTERS_ANY128 = 3 };
 template <typename T, typename TC, bool BKC> static int launch_adapters_form(int form, dim3 grid, hipStream_t s, const AdaptersArgs &a)
 {
     switch (form) {
     case ADAPTERS_128x128: return enqueue(adapters_ring_kernel<T, TC, 128, 128, BKC>, grid, dim3(256), s, a);
     case ADAPTERS_256x256: return enqueue(adapters_ring_kernel<T, TC, 256, 256, BKC>, grid, dim3(256), s, a);
+    case ADAPTERS_ANY128: return enqueue(adapters_any_kernel<T, TC, 128, 128, BKC>, grid, dim3(256), s, a);
     default: return enqueue(adapters_any_kernel<T, TC, 64, 64, BKC>, grid, dim3(256), s, a);
     }
 }

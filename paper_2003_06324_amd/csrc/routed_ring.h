@@ -111,8 +111,7 @@ template <typename T, int R, int NW> struct RingRowsLoader : RingLoader<T, R, NW
     }
 };
 
-// BANDS: block i of a wave is the 32 rows (i * WM + its row of waves) * 32 .. of the tile, so that the waves' i-th blocks are neighbours;
-// otherwise a wave's blocks are.
+// (BANDS as in TileLoop)
 template <typename T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, bool BANDS = false> struct RingLoop {
     static constexpr int NW = WM * WN, NT = NW * 64;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;

@@ -129,7 +129,9 @@ template <typename T, int R, bool KC> __device__ __forceinline__ typename Frag<T
 // has landed (a counted wait), one barrier (by which every wave has read the slab before, so its stage is free), the loads of the slab
 // NST - 1 further, the slab's fragments and matrix instructions.  The caller's at(h) points the loaders to slab h.
 // ---------------------------------------------------------------------------
-template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BKC> struct TileLoop {
+// BANDS: block i of a wave is the 32 rows (i * WM + its row of waves) * 32 .. of the tile, so that the waves' i-th blocks are neighbours;
+// otherwise a wave's blocks are.
+template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BKC, bool BANDS = false> struct TileLoop {
     static constexpr int NW = WM * WN, NT = NW * 64;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     static constexpr int A_BYTES = BM * RBK, B_BYTES = BN * RBK, STAGE = A_BYTES + B_BYTES, LDS_BYTES = NST * STAGE;
@@ -140,6 +142,7 @@ template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BK
     static constexpr int NVA = LoaderA::PER_WAVE, NVB = LoaderB::PER_WAVE, NL = NVA + NVB;
     static_assert((NST - 1) * NL <= 63, "the counted waits go up to 63 loads");
 
+    static __device__ __forceinline__ int row_of(int wm, int i) { return BANDS ? (i * WM + wm) * 32 : wm * TM + i * 32; }
     static __device__ __forceinline__ void zero(float16_t (&acc)[FM][FN])
     {
 #pragma unroll
@@ -159,7 +162,7 @@ template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BK
         for (int kg = 0; kg < KGS; ++kg) {
             frag_t fa[FM], fb[FN];
 #pragma unroll
-            for (int i = 0; i < FM; ++i) fa[i] = Fetch<T, BM, AKC>::get(sA, wm * TM + i * 32, kg, lane);
+            for (int i = 0; i < FM; ++i) fa[i] = Fetch<T, BM, AKC>::get(sA, row_of(wm, i), kg, lane);
 #pragma unroll
             for (int j = 0; j < FN; ++j) fb[j] = Fetch<T, BN, BKC>::get(sB, wn * TN + j * 32, kg, lane);
 #pragma unroll
@@ -185,7 +188,7 @@ template <typename T, int BM, int BN, int WM, int WN, int NST, bool AKC, bool BK
             frag_t fa[FM], fb[FN];
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                fa[i] = Fetch<T, BM, AKC>::get(sA, wm * TM + i * 32, kg, lane);
+                fa[i] = Fetch<T, BM, AKC>::get(sA, row_of(wm, i), kg, lane);
                 if (AKC && kg == krem / KG) fa[i] = __builtin_bit_cast(frag_t, __builtin_bit_cast(uint4_t, fa[i]) & mask);
             }
 #pragma unroll

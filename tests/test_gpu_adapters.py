@@ -86,6 +86,23 @@ def test_strides_and_alignments(kind, pads, shift):
             assert np.array_equal(run(kind, A, B, of, None, down, up, lay, pads, shift), ru.rounded(ref, c))
 
 
+@pytest.mark.parametrize("kind", ["f16f32", "bf16bf16", "f32"])
+@pytest.mark.parametrize("odd", [0, 1])
+@pytest.mark.parametrize("rows,N,K,n,r", [(2100, 2050, 136, 3, 16), (2049, 2048, 70, 5, 72), (4100, 4200, 66, 9, 8),
+                                            (2100, 2050, 1000, 4, 16), (2300, 1601, 999, 3, 70)])
+def test_many_rows(kind, odd, rows, N, K, n, r):
+    """Enough tiles that the chip is full: larger ones, rows on and off 4-byte words; runs of rows, alternating rows, rows without any."""
+    rng = np.random.default_rng(rows + odd)
+    a, c = ru.KINDS[kind]
+    A, B = ru.values(rng, (rows, K), a, "int"), ru.values(rng, (K, N), a, "int")
+    down, up = ru.values(rng, (n, K, r), a, "int") * (rng.random((n, K, r)) < 0.2), np.sign(ru.values(rng, (n, r, N), a, "int"))
+    of = np.repeat(rng.integers(-1, n, size=rows // 150 + 1), 150)[:rows]
+    of[500:700] = np.arange(200) % (n + 1) - 1
+    ref, _, _ = ru.adapters(A, B, of, None, down, up)
+    for lay in ((1, 1, 1), (0, 0, 0)):
+        assert np.array_equal(run(kind, A, B, of, None, down, up, lay, (odd,) * 5), ru.rounded(ref, c))
+
+
 @pytest.mark.parametrize("kind", ["f16f32", "bf16f32", "f32"])
 def test_projections_of_any_size(kind):
     """What lies between the two products is neither cut off at the operand type's largest number nor lost below its smallest."""

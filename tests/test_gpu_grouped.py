@@ -102,6 +102,50 @@ def test_grouped_strides_and_alignments(kind, pads, shift, gap):
                 check(run_grouped(kind, A, offsets, rows, row_map, B, layout, pads, shift, gap), ref, there, mag, kind, K, "int")
 
 
+@pytest.mark.parametrize("kind", ["f16f32", "bf16bf16", "f32"])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_full_chips(kind, odd):
+    """Enough tiles that the chip is full: larger ones, rows on and off 4-byte words."""
+    rng = np.random.default_rng(21 + odd)
+    a, c = ru.KINDS[kind]
+    for G, rows, N, K in ((3, 4000, 2050, 72), (40, 4500, 900, 70)):
+        for layout in LAYOUTS:
+            offsets = cuts(rng, G, rows)
+            A, B = ru.values(rng, (500, K), a, "int"), ru.values(rng, (G, K, N), a, "int")
+            row_map = rng.integers(0, 500, size=rows)
+            ref, there, mag = ru.grouped(A, offsets, rows, row_map, B)
+            check(run_grouped(kind, A, offsets, rows, row_map, B, layout, (odd,) * 3), ref, there, mag, kind, K, "int")
+    for G, rows, M, N in ((5, 700, 1030, 1000), (36, 900, 500, 390)):
+        for layout in LAYOUTS:
+            offsets = cuts(rng, G, rows)
+            A, D = ru.values(rng, (200, M), a, "int"), ru.values(rng, (rows, N), a, "int")
+            row_map = rng.integers(0, 200, size=rows)
+            ref, _ = ru.wgrad(A, offsets, rows, row_map, D)
+            assert np.array_equal(run_wgrad(kind, A, offsets, rows, row_map, D, layout, (odd,) * 3), ru.rounded(ref, c))
+
+
+@pytest.mark.parametrize("kind", ["f16f32", "bf16bf16"])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_long_products_of_odd_rows(kind, layout):
+    """Rows in the middle of 4-byte words in products long enough that they are copied first; called twice, with other operands in
+    between, so that nothing of one call is left for the next."""
+    rng = np.random.default_rng(31)
+    a, c = ru.KINDS[kind]
+    for trial in range(2):
+        for mapped in (False, True):
+            G, rows, N, K = 3, 3000, 1003, 1001
+            offsets = cuts(rng, G, rows, 0.0)
+            A, B = ru.values(rng, (700 if mapped else rows, K), a, "int"), ru.values(rng, (G, K, N), a, "int")
+            row_map = rng.integers(-1, 701, size=rows) if mapped else None
+            ref, there, mag = ru.grouped(A, offsets, rows, row_map, B)
+            check(run_grouped(kind, A, offsets, rows, row_map, B, layout, (0, 2 * trial, 1), (1, 0, 3)), ref, there, mag, kind, K, "int")
+            M = 905
+            A, D = ru.values(rng, (900 if mapped else rows, M), a, "int"), ru.values(rng, (rows, N), a, "int")
+            row_map = rng.integers(-1, 901, size=rows) if mapped else None
+            ref, _ = ru.wgrad(A, offsets, rows, row_map, D)
+            assert np.array_equal(run_wgrad(kind, A, offsets, rows, row_map, D, layout, (0, 0, 2), (1, 0, 0)), ru.rounded(ref, c))
+
+
 def test_grouped_without_rows_columns_or_k():
     rng = np.random.default_rng(5)
     B = ru.values(rng, (3, 8, 16), "f16", "int")
