@@ -62,22 +62,34 @@ template <typename T, typename TC> __global__ __launch_bounds__(COMBINE_THREADS)
     float acc[EL];
 #pragma unroll
     for (int x = 0; x < EL; ++x) acc[x] = 0.0f;
-    for (int j0 = 0; j0 < p.top_k; j0 += AHEAD) {
-        float w[AHEAD], y[AHEAD][EL];
+    const T *const y = (const T *)p.Y + col;
+    for (int j0 = 0; j0 < (p.y_rows > 0 ? p.top_k : 0); j0 += AHEAD) {
+        float w[AHEAD];
         bool there[AHEAD];
+        int64_t at[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int slot = j0 + j < p.top_k ? p.slot_of[t * p.top_k + j0 + j] : -1;
-            there[j] = slot >= 0 && slot < p.y_rows;
-            w[j] = there[j] && p.weights != nullptr ? p.weights[t * p.top_k + j0 + j] : 1.0f;
-            if (there[j]) Piece<T>::load((const T *)p.Y + slot * p.ldy + col, valid, y[j]);
+            const int entry = j0 + j < p.top_k ? j0 + j : p.top_k - 1;
+            const int slot = p.slot_of[t * p.top_k + entry];
+            there[j] = j0 + j < p.top_k && slot >= 0 && slot < p.y_rows;
+            at[j] = (there[j] ? slot : 0) * p.ldy;  // (a slot that is none reads the first row, and is left out below)
+            w[j] = p.weights != nullptr ? p.weights[t * p.top_k + entry] : 1.0f;
         }
+        if (valid == EL) {
+            typename Piece<T>::vec_t v[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-            if (there[j]) {
+            for (int j = 0; j < AHEAD; ++j) v[j] = *(const typename Piece<T>::loose_t *)(y + at[j]);
 #pragma unroll
-                for (int x = 0; x < EL; ++x) acc[x] = fmaf(w[j], y[j][x], acc[x]);
-            }
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int x = 0; x < EL; ++x) acc[x] = there[j] ? fmaf(w[j], (float)v[j][x], acc[x]) : acc[x];
+        } else {
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int x = 0; x < EL; ++x)
+                    if (there[j] && x < valid) acc[x] = fmaf(w[j], (float)y[at[j] + x], acc[x]);
+        }
     }
     TC *o = (TC *)p.out + t * p.ldo + col;
     if constexpr (sizeof(TC) == sizeof(T)) {

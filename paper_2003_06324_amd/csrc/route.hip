@@ -1,6 +1,8 @@
 // Routing to experts: scores, choice and weights, their gradient, and the plan (entries sorted by expert).
 #include "routed_common.h"
 
+#include <algorithm>
+
 using namespace gemm_gfx950;
 
 namespace {
@@ -15,27 +17,127 @@ __device__ __forceinline__ uint32_t order_of(float c)
     return c != c ? 1u : k;
 }
 
+// the number of an order
+__device__ __forceinline__ float number_of(uint32_t k)
+{
+    const float v = __uint_as_float((k >> 31) != 0 ? k & 0x7fffffffu : ~k);
+    return k == 1u ? NAN : v;
+}
+
+// An expert as one number that orders: its choice value's order above, the complement of its index below, in the fraction of a binary64
+// number (2^52 and up), so that one instruction each makes the higher and the lower of two.
+constexpr int INDEX_BITS = 10;  // GEMM_ROUTE_MAX_EXPERTS
+__device__ __forceinline__ double entry_of(uint32_t key, int index)
+{
+    const uint32_t low = key << INDEX_BITS | (((1u << INDEX_BITS) - 1) - (uint32_t)index), high = 0x43300000u | key >> (32 - INDEX_BITS);
+    return __longlong_as_double((long long)((uint64_t)high << 32 | low));
+}
+__device__ __forceinline__ uint32_t key_of(double e)
+{
+    const uint64_t u = (uint64_t)__double_as_longlong(e);
+    return (uint32_t)(u >> INDEX_BITS);
+}
+__device__ __forceinline__ int index_of(double e)
+{
+    return (int)(((1u << INDEX_BITS) - 1) - ((uint32_t)(uint64_t)__double_as_longlong(e) & ((1u << INDEX_BITS) - 1)));
+}
+// (no NaN among them, which fmax would see to)
+__device__ __forceinline__ double higher(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double lower(double a, double b)
+{
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ void compare(double &a, double &b)
+{
+    const double h = higher(a, b);
+    b = lower(a, b);
+    a = h;
+}
+// N numbers into descending order (Batcher's odd-even merge sort)
+template <int N> __device__ __forceinline__ void sort_descending(double (&x)[N])
+{
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i + k < N && i >= k % p && (i - k % p) % (2 * k) < k && i / (2 * p) == (i + k) / (2 * p)) compare(x[i], x[i + k]);
+}
+// the N highest of two descending lists, descending: the higher of opposite places are these, in an order that rises and falls once
+template <int N> __device__ __forceinline__ void merge_descending(double (&x)[N], const double (&other)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = higher(x[i], other[N - 1 - i]);
+#pragma unroll
+    for (int k = N / 2; k >= 1; k /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((i & k) == 0) compare(x[i], x[i + k]);
+}
+template <int S> __device__ __forceinline__ double partner_entry(double e)
+{
+    const uint64_t u = (uint64_t)__double_as_longlong(e);
+    return __longlong_as_double((long long)((uint64_t)partner<S>((uint32_t)(u >> 32)) << 32 | partner<S>((uint32_t)u)));
+}
+template <int L, int N, int S = 0> __device__ __forceinline__ void merge_over(double (&x)[N])
+{
+    if constexpr ((1 << S) < L) {
+        double other[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) other[i] = partner_entry<S>(x[i]);
+        merge_descending<N>(x, other);
+        merge_over<L, N, S + 1>(x);
+    }
+}
+
 template <typename T> __device__ __forceinline__ float as_float(T v) { return (float)v; }
 
 // The V logits of a lane (experts V * lane ..), minus infinity behind the last expert.  WIDE: rows and lanes begin on the boundaries
 // of what a lane reads at once and E is a multiple of V.
-template <typename T, int V, bool WIDE> __device__ __forceinline__ void load_logits(const T *row, int e0, int E, float (&l)[V])
+template <typename T, int V, bool WIDE, int ALIGN = 16> __device__ __forceinline__ void load_logits(const T *row, int e0, int E, float (&l)[V])
 {
     if constexpr (WIDE) {
         constexpr int BYTES = V * (int)sizeof(T);
         constexpr int PIECE = BYTES < 16 ? BYTES : 16, EL = PIECE / (int)sizeof(T);
-        struct alignas(PIECE) piece_t { T v[EL]; };
+        typedef T vec_t __attribute__((ext_vector_type(EL)));
+        typedef vec_t loose_t __attribute__((aligned(PIECE < ALIGN ? PIECE : ALIGN)));
 #pragma unroll
         for (int i = 0; i < V / EL; ++i) {
-            piece_t p;
-            if (e0 < E) p = *(const piece_t *)(row + e0 + i * EL);
+            const vec_t p = *(const loose_t *)(row + (e0 < E ? e0 : 0) + i * EL);  // (E is a multiple of V)
 #pragma unroll
-            for (int x = 0; x < EL; ++x) l[i * EL + x] = e0 < E ? as_float(p.v[x]) : -INFINITY;
+            for (int x = 0; x < EL; ++x) l[i * EL + x] = e0 < E ? as_float(p[x]) : -INFINITY;
         }
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) l[v] = e0 + v < E ? as_float(row[e0 + v]) : -INFINITY;
     }
+}
+
+// e^x: x log2(e) in two parts, cut into a whole number and a rest of at most a half, the instruction's power of the rest (a unit or so in the
+// last place), and the whole number into the exponent, which rounds subnormal results as they should be.
+__device__ __forceinline__ float exp_of(float x)
+{
+    const float log2e = 1.44269504f, more = 1.92596299e-8f;
+    const float y = fminf(fmaxf(x, -200.0f), 200.0f);
+    const float t = y * log2e;
+    const float n = rintf(t);
+    const float e = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((t - n) + fmaf(y, more, fmaf(y, log2e, -t))), (int)n);
+    return x != x ? x : e;
+}
+// 1 / x of a finite x, one Newton step behind the instruction's approximation
+__device__ __forceinline__ float reciprocal(float x)
+{
+    const float r = __builtin_amdgcn_rcpf(x);
+    const float better = fmaf(fmaf(-x, r, 1.0f), r, r);
+    return x == INFINITY ? 0.0f : better;
 }
 
 // Scores of a lane's experts, in place.  Softmax: of a row of nothing but minus infinity zeros; a NaN or plus infinity makes all NaN.
@@ -50,7 +152,7 @@ template <int L, int V> __device__ __forceinline__ void scores(float (&s)[V], bo
         float z = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            s[v] = expf(s[v] - base);
+            s[v] = exp_of(s[v] - base);
             z += s[v];
         }
         z = sum_over<L>(z);
@@ -59,7 +161,7 @@ template <int L, int V> __device__ __forceinline__ void scores(float (&s)[V], bo
         for (int v = 0; v < V; ++v) s[v] = s[v] * d;
     } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) s[v] = 1.0f / (1.0f + expf(-s[v]));
+        for (int v = 0; v < V; ++v) s[v] = reciprocal(1.0f + exp_of(-s[v]));
     }
 }
 
@@ -72,19 +174,20 @@ struct RouteArgs {
     int E, groups, top_groups, group_top, group_size, top_k, softmax, renormalise;
     float scale;
     Divisor by_group;      // group_size
-    int lanes_per_group;   // where a group is this many whole lanes, a power of two; else 0
+    int lanes_per_group, group_shift;  // where a group is this many whole lanes, a power of two (2^group_shift); else 0
 };
 
 // ---------------------------------------------------------------------------
-// L lanes a token, V neighbouring experts a lane.  Scores and choice values stay in registers; a round of the choice is a maximum
-// over the lane's values, one over the lanes, and the lowest index of those that equal it.
-// Bound: reading the logits is little (16384 x 256 in bfloat16: 8 MB, 1.5 us); the instructions of top_k rounds are what it takes,
-// so a token gets as few lanes as its experts fit into the registers of (a wave then works on four at once), and the
-// lanes meet by data-parallel moves instead of shared memory.
+// L lanes a token, V neighbouring experts a lane.  Every lane sorts its experts, and the lanes' lists of the P highest meet in pairs until
+// all of them have the token's; P = 0: more than 16 are chosen, one round after the other.
+// Bound: reading the logits is little (16384 x 256 in bfloat16: 8 MB, 1.5 us); the instructions are what it takes, so a token gets
+// as few lanes as its experts fit into the registers of (a wave then works on four at once), and the lanes meet by
+// data-parallel moves.  Choosing eight of 256 in eight rounds of maxima took 19 us there, with the lists it is 10.8.
 // ---------------------------------------------------------------------------
-template <typename T, int L, int V, bool WIDE>
+template <typename T, int L, int V, int P, bool WIDE>
 __global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
 {
+    __shared__ float score_of[P > 0 ? ROUTE_THREADS * V : 1];
     const int64_t t = ((int64_t)blockIdx.x * ROUTE_THREADS + threadIdx.x) / L;
     const int lane = threadIdx.x % L;
     const bool live = t < p.tokens;   // (a wave's lanes stay together for the moves between them)
@@ -93,35 +196,33 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
     load_logits<T, V, WIDE>((const T *)p.logits + (live ? t : p.tokens - 1) * p.ld, e0, p.E, s);
     scores<L, V>(s, p.softmax != 0);
     uint32_t key[V];
-    float c[V];
+    if (p.bias != nullptr) {
+        float b[V];
+        load_logits<float, V, WIDE, 4>(p.bias, e0, p.E, b);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        c[v] = p.bias != nullptr && e0 + v < p.E ? s[v] + p.bias[e0 + v] : s[v];
-        key[v] = e0 + v < p.E ? order_of(c[v]) : 0u;
+        for (int v = 0; v < V; ++v) key[v] = e0 + v < p.E ? order_of(s[v] + b[v]) : 0u;
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = e0 + v < p.E ? order_of(s[v]) : 0u;
     }
     if (p.groups > 1) {
         // a group's score, in the end in the lane of the group's number
         uint32_t rank = 0;
-        auto two = [&](uint32_t k1, uint32_t k2, float c1, float c2) {
-            // sum of the two highest (one where the group has but one, or one is asked for); NaN if either is
-            return p.group_top == 2 && k2 != 0 ? order_of(c1 + c2) : k1;
-        };
-        // the two highest of a and b, the pairs' order known
-        struct Two { uint32_t k1, k2; float c1, c2; };
-        auto add = [](Two &a, uint32_t k, float v) {
-            const bool first = k > a.k1, second = k > a.k2;
-            a.k2 = first ? a.k1 : (second ? k : a.k2);
-            a.c2 = first ? a.c1 : (second ? v : a.c2);
-            a.k1 = first ? k : a.k1;
-            a.c1 = first ? v : a.c1;
+        // the two highest of a lane's experts of a group, and of several lanes'
+        struct Two { uint32_t k1, k2; };
+        auto add = [](Two &a, uint32_t k) {
+            const uint32_t low = k < a.k1 ? k : a.k1;
+            a.k1 = k > a.k1 ? k : a.k1;
+            a.k2 = low > a.k2 ? low : a.k2;
         };
         auto meet = [&](Two &a, auto step) {
             constexpr int S = decltype(step)::value;
             const uint32_t k1 = partner<S>(a.k1), k2 = partner<S>(a.k2);
-            const float c1 = __uint_as_float(partner<S>(__float_as_uint(a.c1))), c2 = __uint_as_float(partner<S>(__float_as_uint(a.c2)));
-            add(a, k1, c1);
-            add(a, k2, c2);
+            add(a, k1);
+            a.k2 = k2 > a.k2 ? k2 : a.k2;
         };
+        // sum of the two highest (one where the group has but one, or one is asked for); NaN if either is
+        auto two = [&](const Two &a) { return p.group_top == 2 && a.k2 != 0 ? order_of(number_of(a.k1) + number_of(a.k2)) : a.k1; };
         typedef std::integral_constant<int, 0> S0;
         typedef std::integral_constant<int, 1> S1;
         typedef std::integral_constant<int, 2> S2;
@@ -129,9 +230,9 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
         typedef std::integral_constant<int, 4> S4;
         typedef std::integral_constant<int, 5> S5;
         if (p.lanes_per_group > 0) {
-            Two m = {0, 0, 0.0f, 0.0f};
+            Two m = {0, 0};
 #pragma unroll
-            for (int v = 0; v < V; ++v) add(m, key[v], c[v]);
+            for (int v = 0; v < V; ++v) add(m, key[v]);
             const int n = p.lanes_per_group;
             if (n > 1) meet(m, S0());
             if (n > 2) meet(m, S1());
@@ -141,13 +242,13 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
                 if (n > 16) meet(m, S4());
                 if (n > 32) meet(m, S5());
             }
-            const uint32_t mine = two(m.k1, m.k2, m.c1, m.c2);
+            const uint32_t mine = two(m);
             rank = (uint32_t)__shfl((int)mine, lane * n < L ? lane * n : 0, L);
         } else {
             for (int g = 0; g < p.groups; ++g) {
-                Two m = {0, 0, 0.0f, 0.0f};
+                Two m = {0, 0};
 #pragma unroll
-                for (int v = 0; v < V; ++v) add(m, divide(e0 + v, p.by_group) == g ? key[v] : 0u, c[v]);
+                for (int v = 0; v < V; ++v) add(m, divide(e0 + v, p.by_group) == g ? key[v] : 0u);
                 meet(m, S0());
                 meet(m, S1());
                 meet(m, S2());
@@ -156,7 +257,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
                     meet(m, S4());
                     meet(m, S5());
                 }
-                if (lane == g) rank = two(m.k1, m.k2, m.c1, m.c2);
+                if (lane == g) rank = two(m);
             }
         }
         int better = 0;
@@ -165,36 +266,69 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_kernel(const RouteArgs p)
             better += other > rank || (other == rank && g < lane) ? 1 : 0;
         }
         const uint64_t kept = __ballot(lane < p.groups && better < p.top_groups) >> ((threadIdx.x & 63) / L * L);
+        if (p.lanes_per_group > 0) {
+            const bool mine = (kept >> (lane >> p.group_shift)) & 1;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int g = p.lanes_per_group > 0 ? lane / p.lanes_per_group : divide(e0 + v, p.by_group);
-            if (((kept >> (g & 63)) & 1) == 0) key[v] = 0;
+            for (int v = 0; v < V; ++v) key[v] = mine ? key[v] : 0;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = ((kept >> (divide(e0 + v, p.by_group) & 63)) & 1) != 0 ? key[v] : 0;
         }
     }
-    // round j: the winner's index and score end up in lane j
     int my_index = 0;
     float my_score = 0.0f;
-    for (int j = 0; j < p.top_k; ++j) {
-        uint32_t m = key[0];
+    if constexpr (P > 0) {
+        constexpr int HALVES = V > P ? V / P : 1;
+        static_assert(HALVES <= 2, "lists of the higher half");
+        double list[P], more[P];
 #pragma unroll
-        for (int v = 1; v < V; ++v) m = key[v] > m ? key[v] : m;
-        m = umax_over<L>(m);
-        uint32_t at = 0xffffffffu;
-#pragma unroll
-        for (int v = V - 1; v >= 0; --v) at = key[v] == m ? (uint32_t)(e0 + v) : at;
-        at = umin_over<L>(at);
-        float w = 0.0f;
-        uint32_t taken = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const bool it = at == (uint32_t)(e0 + v);
-            taken = it ? __float_as_uint(s[v]) : taken;
-            key[v] = it ? 0u : key[v];
+        for (int i = 0; i < P; ++i) {
+            list[i] = i < V ? entry_of(key[i < V ? i : 0], e0 + i) : 0.0;
+            more[i] = HALVES == 2 ? entry_of(key[HALVES == 2 ? P + i : 0], e0 + P + i) : 0.0;
         }
-        w = __uint_as_float(over_lanes<L>(taken, [](uint32_t a, uint32_t b) { return a | b; }));
-        if (lane == j) {
-            my_index = (int)at;
-            my_score = w;
+        sort_descending<P>(list);
+        if constexpr (HALVES == 2) {
+            sort_descending<P>(more);
+            merge_descending<P>(list, more);
+        }
+        merge_over<L, P>(list);
+        double mine = list[0];
+#pragma unroll
+        for (int i = 1; i < P; ++i) mine = lane == i ? list[i] : mine;
+        my_index = index_of(mine);
+        if (p.bias != nullptr) {  // the choice value is not the score
+            float *const all = score_of + (threadIdx.x / L) * (L * V);
+#pragma unroll
+            for (int v = 0; v < V; ++v) all[e0 + v] = s[v];
+            __syncthreads();
+            my_score = all[lane < p.top_k ? my_index : 0];
+        } else {
+            my_score = number_of(key_of(mine));
+        }
+        if (lane >= p.top_k) my_score = 0.0f;
+    } else {
+        // round j: the winner's index and score end up in lane j
+        for (int j = 0; j < p.top_k; ++j) {
+            uint32_t m = key[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) m = key[v] > m ? key[v] : m;
+            m = umax_over<L>(m);
+            uint32_t at = 0xffffffffu;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) at = key[v] == m ? (uint32_t)(e0 + v) : at;
+            at = umin_over<L>(at);
+            uint32_t taken = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const bool it = at == (uint32_t)(e0 + v);
+                taken = it ? __float_as_uint(s[v]) : taken;
+                key[v] = it ? 0u : key[v];
+            }
+            taken = over_lanes<L>(taken, [](uint32_t a, uint32_t b) { return a | b; });
+            if (lane == j) {
+                my_index = (int)at;
+                my_score = __uint_as_float(taken);
+            }
         }
     }
     float out = my_score * p.scale;
@@ -341,44 +475,74 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_count_kernel(const PlanArgs
     for (int e = threadIdx.x; e < p.E; e += PLAN_THREADS) p.counts[(int64_t)blockIdx.x * p.E + e] = hist[e];
 }
 
-__global__ __launch_bounds__(PLAN_THREADS) void plan_place_kernel(const PlanArgs p)
+// KEEP: the steps are at most two, and a wave keeps its entries in registers
+template <bool KEEP> __global__ __launch_bounds__(PLAN_THREADS) void plan_place_kernel(const PlanArgs p)
 {
-    extern __shared__ int hist[];  // [PLAN_WAVES][E] a wave's next slot per expert, then [PLAN_WAVES] sums
-    int *const sums = hist + PLAN_WAVES * p.E;
+    extern __shared__ int hist[];  // [PLAN_WAVES][E] a wave's next slot per expert; before, shares of the workgroups' counts
+    __shared__ int sums[PLAN_WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    const int64_t first = ((int64_t)blockIdx.x * PLAN_WAVES + wave) * p.steps * 64;
+    int kept[2] = {-1, -1};
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (i < p.steps && first + i * 64 + lane < p.entries) kept[i] = p.indices[first + i * 64 + lane];
+    }
+    // thread e: entries of expert e before this workgroup, and in all of them.  There are more threads than experts as a rule: `shares`
+    // threads an expert add up every shares-th workgroup's counts, and meet in LDS.
+    int before = 0, total = 0;
+    if (gridDim.x > 1) {
+        const int shares = PLAN_THREADS / p.E < 8 ? PLAN_THREADS / p.E : 8, share = tid / p.E, e = tid - share * p.E;
+        if (share < shares) {
+            constexpr int AHEAD = 8;
+            for (int b0 = share; b0 < (int)gridDim.x; b0 += AHEAD * shares) {
+                int c[AHEAD];
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) c[x] = b0 + x * shares < (int)gridDim.x ? p.counts[(int64_t)(b0 + x * shares) * p.E + e] : 0;
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) {
+                    total += c[x];
+                    before += b0 + x * shares < (int)blockIdx.x ? c[x] : 0;
+                }
+            }
+            hist[share * p.E + e] = total;
+            hist[(8 + share) * p.E + e] = before;
+        }
+        __syncthreads();
+        before = total = 0;
+        if (tid < p.E)
+            for (int x = 0; x < shares; ++x) {
+                total += hist[x * p.E + tid];
+                before += hist[(8 + x) * p.E + tid];
+            }
+        __syncthreads();
+    }
     for (int i = tid; i < PLAN_WAVES * p.E; i += PLAN_THREADS) hist[i] = 0;
     __syncthreads();
-    const int64_t first = ((int64_t)blockIdx.x * PLAN_WAVES + wave) * p.steps * 64;
-    count_entries(p, first, lane, hist + wave * p.E);
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (kept[i] >= 0 && kept[i] < p.E) atomicAdd(&hist[wave * p.E + kept[i]], 1);
+    } else {
+        count_entries(p, first, lane, hist + wave * p.E);
+    }
     __syncthreads();
-    // thread e: entries of expert e before this workgroup, and in all of them
-    int before = 0, total = 0;
-    if (tid < p.E) {
-        if (gridDim.x == 1) {
-            for (int w = 0; w < PLAN_WAVES; ++w) total += hist[w * p.E + tid];
-        } else {
-            for (int b = 0; b < (int)gridDim.x; ++b) {
-                const int c = p.counts[(int64_t)b * p.E + tid];
-                before += b < (int)blockIdx.x ? c : 0;
-                total += c;
-            }
-        }
-    }
+    if (tid < p.E && gridDim.x == 1)
+        for (int w = 0; w < PLAN_WAVES; ++w) total += hist[w * p.E + tid];
     // sum of the totals of lower experts
-    int upto = total;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int x = __shfl_up(upto, d);
-        if (lane >= d) upto += x;
-    }
+    const int upto = scan_wave(total);
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    int base = upto - total;
-    for (int w = 0; w < wave; ++w) base += sums[w];
-    int all = 0;
-    for (int w = 0; w < PLAN_WAVES; ++w) all += sums[w];
+    int base = upto - total, all = 0;
+#pragma unroll
+    for (int w = 0; w < PLAN_WAVES; ++w) {
+        base += w < wave ? sums[w] : 0;
+        all += sums[w];
+    }
     if (tid < p.E) {
         if (blockIdx.x == 0) p.offsets[tid] = base;
         int next = base + before;
+#pragma unroll
         for (int w = 0; w < PLAN_WAVES; ++w) {
             const int c = hist[w * p.E + tid];
             hist[w * p.E + tid] = next;
@@ -388,11 +552,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_place_kernel(const PlanArgs
     if (blockIdx.x == 0 && tid == 0) p.offsets[p.E] = all;
     __syncthreads();
     int *const next = hist + wave * p.E;
-    for (int i = 0; i < p.steps; ++i) {
-        const int64_t n = first + i * 64 + lane;
+    auto place = [&](int64_t n, int e) {
         const bool inside = n < p.entries;
-        const int e = inside ? p.indices[n] : -1;
-        const bool valid = e >= 0 && e < p.E;
+        const bool valid = inside && e >= 0 && e < p.E;
         const uint64_t same = same_expert(e, valid, p.bits);
         const int lower = __popcll(same & ((1ull << lane) - 1));
         int slot = -1;
@@ -404,14 +566,30 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_place_kernel(const PlanArgs
         if (valid) p.token_of[slot] = divide((int)n, p.by_k);
         // behind the last slot: as many entries as name no expert, dealt out to the threads
         if (inside && n >= all) p.token_of[n] = -1;
+    };
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (i < p.steps) place(first + i * 64 + lane, kept[i]);
+    } else {
+        for (int i = 0; i < p.steps; ++i) {
+            const int64_t n = first + i * 64 + lane;
+            place(n, n < p.entries ? p.indices[n] : -1);
+        }
     }
 }
 
 template <typename T, int L, int V> int launch_route(const RouteArgs &a, bool wide, hipStream_t s)
 {
     const dim3 grid((unsigned)ceil_div(a.tokens, ROUTE_THREADS / L));
-    return wide ? enqueue(route_kernel<T, L, V, true>, grid, dim3(ROUTE_THREADS), s, a)
-                : enqueue(route_kernel<T, L, V, false>, grid, dim3(ROUTE_THREADS), s, a);
+    if (a.top_k <= 8)
+        return wide ? enqueue(route_kernel<T, L, V, 8, true>, grid, dim3(ROUTE_THREADS), s, a)
+                    : enqueue(route_kernel<T, L, V, 8, false>, grid, dim3(ROUTE_THREADS), s, a);
+    if (a.top_k <= 16)
+        return wide ? enqueue(route_kernel<T, L, V, 16, true>, grid, dim3(ROUTE_THREADS), s, a)
+                    : enqueue(route_kernel<T, L, V, 16, false>, grid, dim3(ROUTE_THREADS), s, a);
+    return wide ? enqueue(route_kernel<T, L, V, 0, true>, grid, dim3(ROUTE_THREADS), s, a)
+                : enqueue(route_kernel<T, L, V, 0, false>, grid, dim3(ROUTE_THREADS), s, a);
 }
 template <typename T, int L, int V> int launch_backward(const RouteBackwardArgs &a, bool wide, hipStream_t s)
 {
@@ -506,8 +684,11 @@ int gemm_route(int elem, int64_t tokens, int64_t experts, const void *logits, in
     const RouteShape r = route_shape(experts, groups, top_k);
     const int size = (int)(experts / groups), lanes = size / r.V;
     RouteArgs a = {logits, bias, weights, indices, tokens, ld, (int)experts, (int)groups, (int)top_groups, group_top, size, (int)top_k,
-                   score == GEMM_SCORE_SOFTMAX, renormalise != 0, scale, divisor(size), 0};
-    if (size % r.V == 0 && lanes > 0 && (lanes & (lanes - 1)) == 0) a.lanes_per_group = lanes;
+                   score == GEMM_SCORE_SOFTMAX, renormalise != 0, scale, divisor(size), 0, 0};
+    if (size % r.V == 0 && lanes > 0 && (lanes & (lanes - 1)) == 0) {
+        a.lanes_per_group = lanes;
+        while ((1 << a.group_shift) < lanes) ++a.group_shift;
+    }
     const bool wide = lanes_wide(logits, ld, experts, r.V, elem == GEMM_ELEM_F32 ? 4 : 2);
     const hipStream_t s = (hipStream_t)hip_stream;
     if (elem == GEMM_ELEM_F32) return route_typed<float>(a, r, wide, s);
@@ -544,12 +725,12 @@ int gemm_route_plan(int64_t tokens, int64_t top_k, int64_t experts, const int32_
     return no_throw([&]() -> int {
         const hipStream_t s = (hipStream_t)hip_stream;
         const int64_t entries = tokens * top_k;
-        // Two launches cost 2 us more than one; a workgroup takes 1024 entries a step and half a microsecond for each.
+        // One workgroup takes 1024 entries a step.  More of them cost another launch (4 us), and read each other's counts: 64 at most.
         const int64_t steps_all = ceil_div(entries, PLAN_THREADS);
         int steps = (int)(steps_all > 0 ? steps_all : 1);
         int blocks = 1;
         if (steps_all > 8) {
-            steps = (int)(steps_all / 64 > 4 ? ceil_div(steps_all, 64) : 4);
+            steps = (int)std::max<int64_t>(2, ceil_div(steps_all, 64));
             blocks = (int)ceil_div(steps_all, steps);
         }
         PlanArgs a = {indices, offsets, token_of, slot_of, nullptr, entries, (int)experts, steps, 0, divisor(top_k)};
@@ -563,8 +744,8 @@ int gemm_route_plan(int64_t tokens, int64_t top_k, int64_t experts, const int32_
             if (hipLaunchKernel((const void *)plan_count_kernel, dim3(blocks), dim3(PLAN_THREADS), argv, experts * sizeof(int), s) != hipSuccess) return GEMM_ERR_HIP;
         }
         void *argv[] = {&a};
-        const size_t lds = (PLAN_WAVES * experts + PLAN_WAVES) * sizeof(int);
-        return hipLaunchKernel((const void *)plan_place_kernel, dim3(blocks), dim3(PLAN_THREADS), argv, lds, s) == hipSuccess ? GEMM_OK : GEMM_ERR_HIP;
+        const void *const kernel = steps <= 2 ? (const void *)plan_place_kernel<true> : (const void *)plan_place_kernel<false>;
+        return hipLaunchKernel(kernel, dim3(blocks), dim3(PLAN_THREADS), argv, PLAN_WAVES * experts * sizeof(int), s) == hipSuccess ? GEMM_OK : GEMM_ERR_HIP;
     });
 }
 

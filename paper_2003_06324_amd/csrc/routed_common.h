@@ -81,6 +81,18 @@ __device__ __forceinline__ void behind_wide_store() { asm volatile("s_nop 1" :::
 // One rounding to 16 bits, to nearest even (NaN stays NaN: both are instructions of gfx950, or what the compiler makes of a cast).
 template <typename T> __device__ __forceinline__ T rounded(float v) { return (T)v; }
 
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int scan_wave(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // one lane further in the row of sixteen
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // last lane of a row to the next row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+    return v;
+}
+
 // ---------------------------------------------------------------------------
 // Reductions over the L lanes that share a token (16, a row of the data-parallel primitives, or a whole wave).  Every lane gets the
 // result; the order of the additions is the same for every lane.

@@ -12,18 +12,6 @@ namespace gemm_gfx950 {
 
 constexpr uint32_t NO_ROW = 0x80000000u;  // an offset past every range: loads of it bring zeros
 
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ int scan_wave(int v)
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // one lane further in the row of sixteen
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // last lane of a row to the next row
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
-    return v;
-}
-
 // A group's rows, as far as they are rows
 struct Span { int lo, hi; };
 __device__ __forceinline__ Span group_span(const int32_t *offsets, int g, int rows)
