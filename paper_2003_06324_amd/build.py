@@ -41,10 +41,10 @@ def _compile(src, force):
 
 def build_binding(force=False):
     """Compile the Python extension that calls the library (host code only). Returns its path."""
-    if force or _stale(BINDING, [BINDING_SRC]):
+    if force or _stale(BINDING, [BINDING_SRC] + glob.glob(os.path.join(INCLUDE, "*.h"))):
         tmp = BINDING + ".tmp%d" % os.getpid()
         subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-                        "-I" + sysconfig.get_paths()["include"], BINDING_SRC, "-o", tmp], check=True,
+                        "-I" + sysconfig.get_paths()["include"], "-I" + INCLUDE, BINDING_SRC, "-o", tmp], check=True,
                        stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
         os.replace(tmp, BINDING)
     return BINDING

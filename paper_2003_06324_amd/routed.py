@@ -5,7 +5,7 @@ the C header, which says what each call computes.
 """
 import ctypes
 
-from .gemm import _check, _ptr, load_library as _load_library
+from .gemm import _binding, _check, _ptr, load_library as _load_library
 
 ELEM_F32, ELEM_F16, ELEM_BF16 = 0, 1, 2
 KIND_BF16BF16 = 4
@@ -25,6 +25,7 @@ SIGNATURES = {
     "gemm_adapters": [_I, _L, _L, _L, _P, _L, _P, _I, _L, _L, _L, _P, _P, _P, _I, _L, _L, _P, _I, _L, _L, _P, _L, _P],
 }
 _bound = None
+_plain = hasattr(_binding, "routed_bind")   # (an extension that was built before these calls leaves them to ctypes)
 
 
 def _lib():
@@ -36,6 +37,8 @@ def _lib():
             fn.argtypes = signature
             fn.restype = ctypes.c_int
         _bound = lib
+        if _plain:
+            _binding.routed_bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in SIGNATURES))
     return _bound
 
 
@@ -94,3 +97,10 @@ def gemm_adapters(kind, rows, N, K, A, lda, B, layoutB, ldb, adapters, rank, ada
     rc = _lib().gemm_adapters(kind, rows, N, K, _ptr(A), lda, _ptr(B), layoutB, ldb, adapters, rank, _ptr(adapter_of), _ptr(scales), _ptr(down),
                               layout_down, ld_down, stride_down, _ptr(up), layout_up, ld_up, stride_up, _ptr(C), ldc, stream or None)
     return _check(rc) if check else rc
+
+
+if _plain:
+    for _i, _name in enumerate(SIGNATURES):
+        _binding.routed_general(_i, globals()[_name])   # before the library is loaded, and for arguments that are not plain
+    from ._binding import (gemm_adapters, gemm_combine, gemm_combine_backward, gemm_grouped, gemm_grouped_wgrad, gemm_route,  # noqa: F811
+                           gemm_route_backward, gemm_route_plan)

@@ -102,3 +102,31 @@ def test_header_is_plain_c(tmp_path):
     src = tmp_path / "use.c"
     src.write_text('#include "gemm_routed.h"\nint kinds(void) { return GEMM_KIND_BF16BF16 + GEMM_SCORE_SIGMOID + GEMM_ELEM_BF16 + GEMM_ADAPTERS_MAX_RANK; }\n')
     subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-fsyntax-only", "-I" + os.path.join(ROOT, "include"), str(src)], check=True)
+
+
+@pytest.mark.parametrize("name", list(CALLS) + ["gemm_route_plan"])
+def test_plain_and_general_calls_agree(name):
+    """The calls through the C extension and the ctypes functions behind it (any keyword argument goes there)."""
+    import inspect
+    fn, plain = getattr(g, name), CALLS.get(name, {**PLAN, "tokens": -1})   # (a plan of no entries still writes its offsets)
+    status = 0 if name in CALLS else INVALID
+    assert list(inspect.signature(fn).parameters) == list(plain) + ["stream", "check"]
+    args = tuple(plain.values())
+    for stream in (0, None):
+        assert fn(*args, stream, False) == status
+        if status == 0:
+            assert fn(*args) == fn(*args, stream) == fn(*args, stream, True) == 0
+    for at in range(0 if status == 0 else 1, len(args)):   # (the plan's first argument is what has it refused)
+        for value in ("x", 1.5j, 2 ** 70):
+            bad = args[:at] + (value,) + args[at + 1:]
+            errors = []
+            for call in (lambda: fn(*bad, 0, False), lambda: fn(*bad, check=False, stream=0)):
+                try:
+                    errors.append(call())
+                except Exception as e:
+                    errors.append(type(e))
+            assert errors[0] == errors[1], (name, at, value, errors)
+    with pytest.raises(TypeError):
+        fn(*args[:-1])
+    with pytest.raises(TypeError):
+        fn(*args, 0, True, 1)
