@@ -728,7 +728,12 @@ int gemm_gfx950::stream_scratch(hipStream_t stream, size_t bytes, StreamScratch 
         if (hipStreamIsCapturing(stream, &status) != hipSuccess) (void)hipGetLastError();
         else if (status == hipStreamCaptureStatusActive) return GEMM_ERR_WORKSPACE;
     }
-    return get_workspace(*dev, stream, bytes, &out.ptr);
+    // (a capture elsewhere in the process need not mind an allocation)
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool exchanged = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+    const int rc = get_workspace(*dev, stream, bytes, &out.ptr);
+    if (exchanged) (void)hipThreadExchangeStreamCaptureMode(&mode);
+    return rc;
 }
 
 namespace {

@@ -1,0 +1,121 @@
+"""A layer of experts on the calls of include/gemm_routed.h, forward, backward and serving with adapters; run as a program it trains a
+small one and serves a batch.
+
+    python -m paper_2003_06324_amd.expert_layer
+
+A token's row x is scored against a router (a plain product), its best experts are chosen, each expert e makes relu(x W1_e) W2_e,
+and the token gets their weighted sum.  The buffers belong to the layer and are those of one batch size; torch owns memory and
+streams and does what is element by element.
+"""
+import torch
+
+import paper_2003_06324_amd as g
+
+
+def _types(dtype):
+    """(kind with results of the same type, kind with binary32 results, element type, product with binary32 results)"""
+    return {torch.float32: (g.KIND_F32, g.KIND_F32, g.ELEM_F32, g.gemm_f32),
+            torch.float16: (g.KIND_F16F16, g.KIND_F16F32, g.ELEM_F16, g.gemm_f16f32),
+            torch.bfloat16: (g.KIND_BF16BF16, g.KIND_BF16F32, g.ELEM_BF16, g.gemm_bf16f32)}[dtype]
+
+
+class ExpertLayer:
+    def __init__(self, tokens, width, hidden, experts, top_k, dtype=torch.bfloat16, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.tokens, self.width, self.hidden, self.experts, self.top_k, self.dtype = tokens, width, hidden, experts, top_k, dtype
+        self.kind, self.kind32, self.elem, self.product = _types(dtype)
+
+        def weights(*shape):
+            return (torch.randn(shape, generator=gen, device="cuda") * shape[-1] ** -0.5).to(dtype)
+        # stored as the columns of the right operand, one after the other (column-major)
+        self.router, self.w1, self.w2 = weights(experts, width), weights(experts, hidden, width), weights(experts, width, hidden)
+        self.masters = None   # the weights in binary32, for training
+        rows = tokens * top_k
+
+        def room(*shape, type=dtype):
+            return torch.empty(shape, dtype=type, device="cuda")
+        self.logits, self.weights = room(tokens, experts, type=torch.float32), room(tokens, top_k, type=torch.float32)
+        self.indices, self.slot_of = room(tokens, top_k, type=torch.int32), room(tokens, top_k, type=torch.int32)
+        self.offsets, self.token_of = room(experts + 1, type=torch.int32), room(rows, type=torch.int32)
+        self.mid, self.act, self.y, self.out = room(rows, hidden), room(rows, hidden), room(rows, width), room(tokens, width)
+        self.d_y, self.d_act, self.d_rows, self.dx = room(rows, width), room(rows, hidden), room(rows, width), room(tokens, width)
+        self.d_weights, self.d_logits = room(tokens, top_k, type=torch.float32), room(tokens, experts, type=torch.float32)
+        self.dx_router, self.d_router = room(tokens, width, type=torch.float32), room(experts, width, type=torch.float32)
+        self.d_w1, self.d_w2 = (room(*w.shape, type=torch.float32) for w in (self.w1, self.w2))
+
+    def forward(self, x):
+        T, D, F, E, k, rows = self.tokens, self.width, self.hidden, self.experts, self.top_k, self.tokens * self.top_k
+        stream = torch.cuda.current_stream().cuda_stream
+        self.x = x
+        self.product(T, E, D, x, g.ROW_MAJOR, 0, self.router, g.COL_MAJOR, 0, self.logits, g.ROW_MAJOR, 0, stream)
+        g.gemm_route(g.ELEM_F32, T, E, self.logits, 0, None, g.SCORE_SOFTMAX, 1, 1, 1, k, 1, 1.0, self.weights, self.indices, stream)
+        g.gemm_route_plan(T, k, E, self.indices, self.offsets, self.token_of, self.slot_of, stream)
+        g.gemm_grouped(self.kind, E, self.offsets, rows, F, D, x, T, 0, self.token_of, self.w1, g.COL_MAJOR, 0, 0, self.mid, 0, stream)
+        torch.clamp(self.mid, min=0, out=self.act)
+        g.gemm_grouped(self.kind, E, self.offsets, rows, D, F, self.act, rows, 0, None, self.w2, g.COL_MAJOR, 0, 0, self.y, 0, stream)
+        g.gemm_combine(self.kind, T, k, D, self.y, rows, 0, self.slot_of, self.weights, self.out, 0, stream)
+        return self.out
+
+    def backward(self, d_out):
+        """Gradients of the last forward(): of x, and in d_router, d_w1, d_w2 (binary32) of the weights."""
+        T, D, F, E, k, rows = self.tokens, self.width, self.hidden, self.experts, self.top_k, self.tokens * self.top_k
+        stream = torch.cuda.current_stream().cuda_stream
+        g.gemm_combine_backward(self.elem, T, k, D, d_out, 0, self.y, rows, 0, self.slot_of, self.weights, self.d_y, 0, self.d_weights, stream)
+        # a product's gradients: for its rows the same product with the other layout, for its matrices the rows' own
+        g.gemm_grouped_wgrad(self.kind32, E, self.offsets, rows, F, D, self.act, rows, 0, None, self.d_y, 0, self.d_w2, g.COL_MAJOR, 0, 0, stream)
+        g.gemm_grouped(self.kind, E, self.offsets, rows, F, D, self.d_y, rows, 0, None, self.w2, g.ROW_MAJOR, 0, 0, self.d_act, 0, stream)
+        self.d_act.mul_(self.mid > 0)
+        g.gemm_grouped_wgrad(self.kind32, E, self.offsets, rows, D, F, self.x, T, 0, self.token_of, self.d_act, 0, self.d_w1, g.COL_MAJOR, 0, 0, stream)
+        g.gemm_grouped(self.kind, E, self.offsets, rows, D, F, self.d_act, rows, 0, None, self.w1, g.ROW_MAJOR, 0, 0, self.d_rows, 0, stream)
+        g.gemm_combine(self.kind, T, k, D, self.d_rows, rows, 0, self.slot_of, None, self.dx, 0, stream)
+        # the router's share
+        g.gemm_route_backward(g.ELEM_F32, T, E, self.logits, 0, g.SCORE_SOFTMAX, k, 1, 1.0, self.indices, self.d_weights, self.d_logits, 0, stream)
+        d = self.d_logits.to(self.dtype)
+        self.product(E, D, T, d, g.COL_MAJOR, 0, self.x, g.ROW_MAJOR, 0, self.d_router, g.ROW_MAJOR, 0, stream)
+        self.product(T, D, E, d, g.ROW_MAJOR, 0, self.router, g.ROW_MAJOR, 0, self.dx_router, g.ROW_MAJOR, 0, stream)
+        return self.dx.add_(self.dx_router)
+
+    def step(self, rate):
+        weights = (self.router, self.w1, self.w2)
+        if self.masters is None:
+            self.masters = [w.float() for w in weights]
+        for w, master, d in zip(weights, self.masters, (self.d_router, self.d_w1, self.d_w2)):
+            w.copy_(master.sub_(d, alpha=rate))
+
+    def serve(self, x, projection, adapter_of, down, up):
+        """forward() of a shared projection of x, with the adapters of the requests that the rows belong to (-1: none):
+        projection width x width, down adapters x rank x width, up adapters x width x rank."""
+        stream = torch.cuda.current_stream().cuda_stream
+        h = torch.empty_like(x)
+        g.gemm_adapters(self.kind, self.tokens, self.width, self.width, x, 0, projection, g.COL_MAJOR, 0, down.shape[0], down.shape[1], adapter_of, None,
+                        down, g.COL_MAJOR, 0, 0, up, g.COL_MAJOR, 0, 0, h, 0, stream)
+        return self.forward(h)
+
+
+def main(steps=60, tokens=512, width=256, hidden=512, experts=16, top_k=2):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    teacher = ExpertLayer(tokens, width, hidden, experts, top_k, seed=7)
+    layer = ExpertLayer(tokens, width, hidden, experts, top_k, seed=8)
+    layer.router.copy_(teacher.router)
+    losses = []
+    for step in range(steps):
+        x = torch.randn((tokens, width), generator=gen, device="cuda").to(layer.dtype)
+        miss = layer.forward(x).float() - teacher.forward(x).float()
+        losses.append(miss.square().mean().item())
+        layer.backward((miss * (2.0 / tokens)).to(layer.dtype))
+        layer.step(0.1)
+        if step % 10 == 0 or step == steps - 1:
+            print("step %3d  mean square miss %.4f" % (step, losses[-1]), flush=True)
+    x = torch.randn((tokens, width), generator=gen, device="cuda").to(layer.dtype)
+    eye = torch.eye(width, device="cuda").to(layer.dtype)
+    down, up = (torch.randn(shape, generator=gen, device="cuda").to(layer.dtype) * 0.1 for shape in ((4, 8, width), (4, width, 8)))
+    of = torch.randint(-1, 4, (tokens,), generator=gen, device="cuda").int()
+    plain = layer.forward(x).clone()
+    adapted = layer.serve(x, eye, of, down, up)
+    print("served %d rows, %d of them adapted; rows without an adapter as before: %s" % (
+        tokens, int((of >= 0).sum()), bool(torch.equal(adapted[of < 0], plain[of < 0]))), flush=True)
+    return losses
+
+
+if __name__ == "__main__":
+    main()
