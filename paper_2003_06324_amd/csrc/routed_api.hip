@@ -154,7 +154,7 @@ template <size_t N> int copy_packed(const Packing (&pack)[N], hipStream_t s)
 // 2048 x 2047, 512 rows each 404 and 441 us; 128 of 2047 x 1536, 4 rows each 196 and 155).
 bool any_large(int64_t tiles128, int64_t num_cu) { return tiles128 >= num_cu; }
 
-// Tile of the weight gradients, by the rounds that the chip takes (see grouped_form; 32 matrices of 2048 x 1024, 1024 rows each 155 us on
+// Tile of the weight gradients, by the rounds that the chip takes (see grouped_form; 32 matrices of 2048 x 1024, 1024 rows each 164 us on
 // 256 x 256, 220 on 128 x 128).
 int wgrad_form(int64_t groups, int64_t M, int64_t N, int64_t num_cu)
 {
@@ -252,7 +252,7 @@ int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t
             if (rc != GEMM_OK) return rc;
         }
         // The kernels write rows of C: a column-major C is the row-major C^T = D^T A.
-        WgradArgs a = {A, D, C, offsets, row_map, nullptr, lda, ldd, ldc, strideC, (int)groups, (int)rows, (int)a_rows, (int)rows, (int)M, (int)N, 0, 0, 0};
+        WgradArgs a = {A, D, C, offsets, row_map, nullptr, lda, ldd, ldc, strideC, (int)groups, (int)rows, (int)a_rows, (int)rows, (int)M, (int)N, 0, 0, 0, 1};
         // C is written once; from 256 rows a group on it pays to keep it from displacing the rows in the L2 (32 matrices of 2048 x 1024 in
         // binary32, 1024 rows each 198 -> 180 us; 64 rows each 62 -> 69)
         a.stream = rows >= 256 * groups;
@@ -269,7 +269,8 @@ int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t
         const int64_t edge = form == WGRAD_ANY ? 64 : (form == WGRAD_256x256 ? 256 : 128);
         a.tiles_m = (int)ceil_div(a.M, edge);
         a.tiles_n = (int)ceil_div(a.N, edge);
-        const int64_t grid = wgrad_grid(groups, rows, (int64_t)a.tiles_m * a.tiles_n);
+        const int64_t tiles = groups * a.tiles_m * a.tiles_n, grid = wgrad_grid(tiles);
+        a.run = wgrad_run(tiles);
         if (grid > (1LL << 24) - 1) return GEMM_ERR_UNSUPPORTED;
         const int rc = copy_packed(pack, s);
         if (rc != GEMM_OK) return rc;

@@ -12,6 +12,7 @@ struct WgradArgs {
     int64_t ldx, ldy, ldc, strideC;
     int groups, rows, x_rows, y_rows, M, N, tiles_m, tiles_n;
     int stream;  // C is stored past the L2
+    int run;     // wgrad_run()
 };
 
 // Direct loads of an operand whose k-rows are a group's rows.  Without a map its base moves from slab to slab.  With one the lanes' offsets
@@ -131,57 +132,33 @@ template <typename T, int R, int NW, bool MAPPED> struct RingKRowsLoader : RingL
     }
 };
 
-// What a tile's start and store weigh, in slabs of 64 rows.
-constexpr int WGRAD_TILE = 8;
-// workgroups of a launch: as many tiles as can fall into an eighth of the weight, for each XCD
-static inline int64_t wgrad_grid(int64_t groups, int64_t rows, int64_t per)
-{
-    const int64_t weight = per * (rows / 64 + groups * (1 + WGRAD_TILE));  // at most
-    const int64_t most = ceil_div(ceil_div(weight, 8), WGRAD_TILE) + 1;
-    return 8 * (most < per * groups ? most : per * groups);
-}
-// Tile of this workgroup.  Tiles are numbered matrix by matrix and take as long as their group has rows, so the XCDs get contiguous runs of
-// the same weight, not of the same number.
+// Tiles in a row that one XCD takes: they are neighbours in their matrix and share panels in its L2.  While all tiles run at once their order
+// is no matter and an XCD gets one run of them.
+constexpr int WGRAD_RUN = 8;
+static inline int wgrad_run(int64_t tiles) { return tiles > 64 * WGRAD_RUN ? WGRAD_RUN : (int)ceil_div(tiles, 8); }
+static inline int64_t wgrad_grid(int64_t tiles) { return ceil_div(tiles, 8 * wgrad_run(tiles)) * 8 * wgrad_run(tiles); }
+// Tile of this workgroup.  A tile takes as long as its group has rows, so the longest are dealt first and the XCDs get runs of the same
+// length in turn: what is left at the end is short.  (Groups are ordered 64 at a time.)
 __device__ __forceinline__ bool wgrad_tile(const WgradArgs &p, int lane, int &group, int &tile_m, int &tile_n)
 {
     const uint32_t per = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n;
-    auto weight_of = [&](int g) {  // of one tile
-        if (g >= p.groups) return 0;
-        const Span s = group_span(p.offsets, g, p.rows);
-        return (s.hi - s.lo + 63) / 64 + WGRAD_TILE;
-    };
-    int total = 0;
-    for (int c = 0; c < p.groups; c += 64) total += __builtin_amdgcn_readlane(scan_wave(weight_of(c + lane)), 63);
-    // the tiles whose beginnings lie in [from, to) of the weight; the i-th of them
-    const uint64_t all = (uint64_t)(uint32_t)total * per, share = (all + 7) / 8;
-    const uint64_t from = share * (blockIdx.x & 7), to = from + share;
-    uint32_t i = blockIdx.x >> 3;
-    uint64_t before = 0;
-    for (int c = 0; c < p.groups; c += 64) {
-        const int w = weight_of(c + lane);
-        const int upto = scan_wave(w);
-        const uint64_t begin = before + (uint64_t)(uint32_t)(upto - w) * per, end = before + (uint64_t)(uint32_t)upto * per;
-        // this lane's group: its tiles [first, last) are the XCD's
-        uint32_t first = 0, last = 0;
-        if (w > 0 && begin < to && end > from) {
-            first = begin >= from ? 0 : (uint32_t)((from - begin + w - 1) / w);
-            last = end <= to ? per : (uint32_t)((to - begin + w - 1) / w);
-        }
-        const int mine = last > first ? (int)(last - first) : 0;
-        const int sum = scan_wave(mine);
-        const uint64_t past = __ballot((uint32_t)sum > i);
-        if (past != 0) {
-            const int at = __builtin_ctzll(past);
-            group = c + at;
-            const uint32_t in = i - (uint32_t)(__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at)) + (uint32_t)__builtin_amdgcn_readlane((int)first, at);
-            tile_n = __builtin_amdgcn_readfirstlane((int)(in / (uint32_t)p.tiles_m));
-            tile_m = __builtin_amdgcn_readfirstlane((int)(in - (uint32_t)tile_n * (uint32_t)p.tiles_m));
-            return true;
-        }
-        i -= (uint32_t)__builtin_amdgcn_readlane(sum, 63);
-        before += (uint64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * per;
+    const uint32_t run = (uint32_t)p.run, turn = blockIdx.x >> 3, runs = turn / run;
+    const uint32_t t = (runs * 8 + (blockIdx.x & 7)) * run + (turn - runs * run);
+    const uint32_t place = t / per, in = t - place * per;
+    if (place >= (uint32_t)p.groups) return false;
+    const int c = (int)(place & ~63u), n = p.groups - c < 64 ? p.groups - c : 64;
+    int slabs = -1;
+    if (lane < n) {
+        const Span s = group_span(p.offsets, c + lane, p.rows);
+        slabs = (s.hi - s.lo + 63) / 64;
     }
-    return false;
+    const int key = slabs * 64 + (63 - lane);  // of equal ones the first comes first
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
+    group = c + __builtin_ctzll(__ballot(lane < n && rank == (int)(place & 63)));
+    tile_n = __builtin_amdgcn_readfirstlane((int)(in / (uint32_t)p.tiles_m));
+    tile_m = __builtin_amdgcn_readfirstlane((int)(in - (uint32_t)tile_n * (uint32_t)p.tiles_m));
+    return true;
 }
 
 // MAPPED: 0 no map, 1 X's rows are gathered, 2 Y's
