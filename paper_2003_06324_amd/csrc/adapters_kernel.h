@@ -25,7 +25,7 @@ struct AdaptersArgs {
     int tiles_m, tiles_n;
     Divisor by_band, by_last_rows;
     float *t;               // T's slices, [t_slices][rows][t_pitch]
-    int t_pitch, t_slices, t_k, turns;  // t_k: k of a slice; turns: see down_slice
+    int t_pitch, t_slices, t_k, turns, rank_tiles;  // t_k: k of a slice; turns, rank_tiles: see down_slice
     // few rows
     float *part;            // the product's slices, [slices][rows][part_pitch]
     int part_pitch, slices, k_slice;
@@ -51,15 +51,17 @@ __device__ __forceinline__ uint32_t next_adapter(int id, int above, uint32_t tur
 }
 
 // ---------------------------------------------------------------------------
-// Slices of T straight from memory to the matrix instructions, any alignment: a wave takes 32 rows, a slice of K, and of the adapters that
-// the rows have those whose number is its turn's.  Wave `item` of row tiles x slices x turns.  KC: down is K-contiguous.
+// Slices of T straight from memory to the matrix instructions, any alignment: a wave takes 32 rows, 32 columns of rank, a slice of K, and of
+// the adapters that the rows have those whose number is its turn's.  Wave `item` of row tiles x slices x turns x rank_tiles.  KC: down is
+// K-contiguous.
 // ---------------------------------------------------------------------------
 template <typename T, bool KC> __device__ __forceinline__ void down_slice(const AdaptersArgs &p, int item, int lane)
 {
     constexpr int KG = Elem<T>::KG, EPL = KG / 2, AHEAD = 8;
     typedef typename Frag<T>::type frag_t;
-    const uint32_t turn = (uint32_t)item % (uint32_t)p.turns;
-    const int rest = item / p.turns, slice = rest % p.t_slices, m0 = rest / p.t_slices * DOWN_ROWS;
+    const int q0 = item % p.rank_tiles * 32, by_turn = item / p.rank_tiles;
+    const uint32_t turn = (uint32_t)by_turn % (uint32_t)p.turns;
+    const int rest = by_turn / p.turns, slice = rest % p.t_slices, m0 = rest / p.t_slices * DOWN_ROWS;
     if (m0 >= p.rows) return;
     const int k0 = slice * p.t_k, k1 = k0 + p.t_k < p.K ? k0 + p.t_k : p.K;
     const int id = adapter_at(p, m0 + (lane & 31));
@@ -71,37 +73,35 @@ template <typename T, bool KC> __device__ __forceinline__ void down_slice(const 
         a = __builtin_amdgcn_readfirstlane((int)next);
         const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
         const T *const down = (const T *)p.down + (int64_t)a * p.stride_down;
-        for (int q0 = 0; q0 < p.rank; q0 += 32) {
-            const int q = q0 + (lane & 31) < p.rank ? q0 + (lane & 31) : p.rank - 1;
-            float16_t acc;
+        const int q = q0 + (lane & 31) < p.rank ? q0 + (lane & 31) : p.rank - 1;
+        float16_t acc;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-            // the operands of eight k-groups are asked for before the first is multiplied
-            int k = k0;
-            for (; k + AHEAD * KG <= k1; k += AHEAD * KG) {
-                frag_t fa[AHEAD], fb[AHEAD];
+        for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+        // the operands of eight k-groups are asked for before the first is multiplied
+        int k = k0;
+        for (; k + AHEAD * KG <= k1; k += AHEAD * KG) {
+            frag_t fa[AHEAD], fb[AHEAD];
 #pragma unroll
-                for (int x = 0; x < AHEAD; ++x) {
-                    const int kl = k + x * KG + (lane >> 5) * EPL;
-                    fa[x] = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, true);
-                    fb[x] = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, true);
-                }
-#pragma unroll
-                for (int x = 0; x < AHEAD; ++x) mma(acc, fa[x], fb[x]);
-            }
-            for (; k < k1; k += KG) {
-                const int kl = k + (lane >> 5) * EPL;
-                const bool full = k + KG <= p.K;
-                const frag_t fa = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, full);
-                const frag_t fb = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, full);
-                mma(acc, fa, fb);
+            for (int x = 0; x < AHEAD; ++x) {
+                const int kl = k + x * KG + (lane >> 5) * EPL;
+                fa[x] = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, true);
+                fb[x] = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, true);
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int x = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-                const int of = __shfl(id, x);  // (by all lanes)
-                if (of == a && q0 + (lane & 31) < p.rank) p.t[((int64_t)slice * p.rows + m0 + x) * p.t_pitch + q0 + (lane & 31)] = scale * acc[r];
-            }
+            for (int x = 0; x < AHEAD; ++x) mma(acc, fa[x], fb[x]);
+        }
+        for (; k < k1; k += KG) {
+            const int kl = k + (lane >> 5) * EPL;
+            const bool full = k + KG <= p.K;
+            const frag_t fa = small_fragment<T, true>((const T *)p.A, p.lda, row, kl, p.K, full);
+            const frag_t fb = small_fragment<T, KC>(down, p.ld_down, q, kl, p.K, full);
+            mma(acc, fa, fb);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int x = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+            const int of = __shfl(id, x);  // (by all lanes)
+            if (of == a && q0 + (lane & 31) < p.rank) p.t[((int64_t)slice * p.rows + m0 + x) * p.t_pitch + q0 + (lane & 31)] = scale * acc[r];
         }
     }
 }
@@ -395,9 +395,18 @@ template <typename T, int BM, int BN, int NST, bool KC> __global__ __launch_boun
 // Rows of other adapters take part in a product and are not taken over: masked to zeros they would meet the adapter's matrix
 // all the same, and a NaN or an infinity in it would reach them.
 // ---------------------------------------------------------------------------
+struct RowOf {  // adapter of a thread's row of the tile, and the factor of its parts: asked for before the K loop
+    int id;
+    float scale;
+    template <typename T> __device__ __forceinline__ void ask(const AdaptersArgs &p, int row)
+    {
+        id = adapter_at(p, row);
+        scale = std::is_same<T, _Float16>::value && p.adapters > 0 ? p.t_scale[row < p.rows ? row : 0] : 1.0f;  // (of a row without adapter: not used)
+    }
+};
 template <typename T, typename TC, int BM, int BN, int WM, int WN, int LDS_BYTES>
-__device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(char) * lds, float16_t (&acc)[BM / WM / 32][BN / WN / 32], int m0, int n0, int tid,
-                                              int wave, int lane)
+__device__ __forceinline__ void add_and_store(const AdaptersArgs &p, const RowOf &own, GEMM_LDS(char) * lds, float16_t (&acc)[BM / WM / 32][BN / WN / 32], int m0,
+                                              int n0, int tid, int wave, int lane)
 {
     typedef typename Frag<T>::type frag_t;
     constexpr int NT = WM * WN * 64, BK = Elem<T>::BK, KG = Elem<T>::KG, NP = Parts<T>::N;
@@ -416,29 +425,32 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
     GEMM_LDS(float) *stage = (GEMM_LDS(float) *)(lds + AT_STAGE + wave * (32 * SW * 4));
     const int wm = wave / WN, wn = wave % WN, rows = p.rows - m0, cols = p.N - n0;
     // T's rows of a band: whole granules, one row of threads for each of the parts
-    auto stage_t = [&](int band, int q0) {
-        constexpr int ITERS = BAND * GPR / NT;
-        uint4_t v[NP][ITERS];
+    constexpr int ITERS = BAND * GPR / NT;
+    uint4_t t_next[NP][ITERS];
+    auto fetch_t = [&](int band, int q0) {
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {
             const int x = (tid + i * NT) / GPR, g = tid % GPR, row = m0 + band * BAND + x;
             const T *const t = (const T *)p.t_parts + (int64_t)(row < p.rows ? row : p.rows - 1) * NP * p.t_pitch + q0 + g * Elem<T>::EPC;
 #pragma unroll
-            for (int n = 0; n < NP; ++n) v[n][i] = *(const uint4_t *)(t + n * p.t_pitch);
+            for (int n = 0; n < NP; ++n) t_next[n][i] = *(const uint4_t *)(t + n * p.t_pitch);
         }
+    };
+    auto store_t = [&]() {
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {
             const int x = (tid + i * NT) / GPR, g = tid % GPR;
 #pragma unroll
-            for (int n = 0; n < NP; ++n) *(GEMM_LDS(uint4_t) *)(lds + AT_T + n * T_BYTES + x * RBK + ((g ^ swz_kc(x)) << 4)) = v[n][i];
+            for (int n = 0; n < NP; ++n) *(GEMM_LDS(uint4_t) *)(lds + AT_T + n * T_BYTES + x * RBK + ((g ^ swz_kc(x)) << 4)) = t_next[n][i];
         }
     };
     const bool at_once = p.rank <= BK;  // T's and the up matrices' images hold all of rank
+    if (p.adapters > 0 && at_once) fetch_t(0, 0);
     __syncthreads();  // every wave has read its last operands
-    for (int r = tid; r < BM; r += NT) {
-        const int a = adapter_at(p, m0 + r);
-        ids[r] = a;
-        scale[r] = std::is_same<T, _Float16>::value && a >= 0 ? p.t_scale[m0 + r] : 1.0f;
+    static_assert(BM <= NT, "a row a thread");
+    if (tid < BM) {
+        ids[tid] = own.id;
+        scale[tid] = own.id >= 0 ? own.scale : 1.0f;
     }
     __syncthreads();
     int held[2] = {-1, -1}, victim = 0;  // adapters whose up matrices are there (all of rank)
@@ -453,11 +465,11 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
             return (int)__builtin_amdgcn_readfirstlane((int)umin_over<64>(next));
         };
         int a = p.adapters > 0 ? next_of(-1) : -1;
-        if (at_once && a != -1) stage_t(i, 0);
+        bool t_there = false;  // T's image is the band's
         while (a != -1) {
             const T *const up = (const T *)p.up + (int64_t)a * p.stride_up;
             for (int q0 = 0; q0 < p.rank; q0 += BK) {
-                if (!at_once) stage_t(i, q0);
+                if (!at_once) fetch_t(i, q0);
                 int slot = at_once && held[0] == a ? 0 : (at_once && NU == 2 && held[1] == a ? 1 : -1);
                 if (slot < 0) {
                     slot = victim;
@@ -475,6 +487,8 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
                         u.store(img, tid);
                     }
                 }
+                if (!at_once || !t_there) store_t();  // (asked for before the up matrix)
+                t_there = true;
                 const GEMM_LDS(char) *const img = lds + slot * U_BYTES;
                 __syncthreads();
                 float16_t add[FN];
@@ -506,6 +520,7 @@ __device__ __forceinline__ void add_and_store(const AdaptersArgs &p, GEMM_LDS(ch
             }
             a = next_of(a);
         }
+        if (p.adapters > 0 && at_once && i + 1 < FM) fetch_t(i + 1, 0);
         // (a wave's staging area is its own)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
@@ -574,10 +589,12 @@ __global__ __launch_bounds__(256) void adapters_ring_kernel(const AdaptersArgs p
     RingLoader<T, BN, 4, BKC> lb;
     la.init((const T *)p.A, p.lda, m0, p.rows, wave, lane);
     lb.init((const T *)p.B, p.ldb, n0, p.N, wave, lane);
+    RowOf own;
+    own.ask<T>(p, tid < BM ? m0 + tid : p.rows);
     float16_t acc[Loop::FM][Loop::FN];
     Loop::run(la, lb, DirectLoader<T, BM, 4, true>::end_of((const T *)p.A, p.lda, p.rows, p.K), DirectLoader<T, BN, 4, BKC>::end_of((const T *)p.B, p.ldb, p.N, p.K),
               krem < Loop::BK || lb.reaches_end(n0, p.N), n, krem, lds, acc, wave, lane);
-    add_and_store<T, TC, BM, BN, 2, 2, Loop::LDS_BYTES>(p, lds, acc, m0, n0, tid, wave, lane);
+    add_and_store<T, TC, BM, BN, 2, 2, Loop::LDS_BYTES>(p, own, lds, acc, m0, n0, tid, wave, lane);
 }
 
 // The same through registers: any alignment, any leading dimension.
@@ -591,10 +608,12 @@ __global__ __launch_bounds__(256) void adapters_any_kernel(const AdaptersArgs p)
     int tile_m, tile_n;
     if (!adapters_tile(p, tile_m, tile_n)) return;
     const int m0 = tile_m * BM, n0 = tile_n * BN;
+    RowOf own;
+    own.ask<T>(p, tid < BM ? m0 + tid : p.rows);
     float16_t acc[Loop::FM][Loop::FN];
     Loop::zero(acc);
     granule_product<T, Loop, BM, BN, BKC>((const T *)p.A, p.lda, (const T *)p.B, p.ldb, m0, p.rows, n0, p.N, 0, p.K, lds, acc, tid, wave, lane);
-    add_and_store<T, TC, BM, BN, 2, 2, Loop::LDS_BYTES>(p, lds, acc, m0, n0, tid, wave, lane);
+    add_and_store<T, TC, BM, BN, 2, 2, Loop::LDS_BYTES>(p, own, lds, acc, m0, n0, tid, wave, lane);
 }
 
 }  // namespace gemm_gfx950

@@ -313,6 +313,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         a.lda = lda, a.ldb = ldb, a.ldc = ldc, a.ld_down = ld_down, a.stride_down = stride_down, a.ld_up = ld_up, a.stride_up = stride_up;
         a.rows = (int)rows, a.N = (int)N, a.K = (int)K, a.adapters = some ? (int)adapters : 0, a.rank = (int)rank;
         a.up_kc = layout_up == GEMM_COL_MAJOR;
+        a.rank_tiles = (int)ceil_div(rank, 32);
         const bool fast = direct(A, lda, 0, esz) && direct(B, ldb, 0, esz);
         StreamScratch scratch;
         const int state = stream_scratch(s, 0, scratch);
@@ -337,7 +338,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
                 const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(num_cu / row_tiles, JOIN_T / rank), K / 256));
                 a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
                 a.t_slices = (int)ceil_div(K, a.t_k);
-                a.down_groups = (int)ceil_div(row_tiles * a.t_slices * a.turns, DOWN_WAVES);
+                a.down_groups = (int)ceil_div(row_tiles * a.t_slices * a.turns * a.rank_tiles, DOWN_WAVES);
             }
             const size_t t_bytes = (size_t)a.t_slices * rows * a.t_pitch * sizeof(float);
             const int rc = stream_scratch(s, t_bytes + (size_t)a.slices * rows * a.part_pitch * sizeof(float) + 256, scratch);
@@ -387,7 +388,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
             a.t = (float *)at;
             a.t_parts = at + t_bytes;
             a.t_scale = (float *)(at + t_bytes + part_bytes);
-            const dim3 grid((unsigned)ceil_div(row_tiles * a.t_slices, fast_down ? 1 : DOWN_WAVES)), sums((unsigned)ceil_div(rows, 32));
+            const dim3 grid((unsigned)fast_down ? row_tiles * a.t_slices : ceil_div(row_tiles * a.t_slices * a.rank_tiles, DOWN_WAVES)), sums((unsigned)ceil_div(rows, 32));
             int sent = elem == GEMM_ELEM_F32   ? launch_adapters_down<float>(dkc, fast_down, grid, s, a)
                        : elem == GEMM_ELEM_F16 ? launch_adapters_down<_Float16>(dkc, fast_down, grid, s, a)
                                                : launch_adapters_down<__bf16>(dkc, fast_down, grid, s, a);

@@ -79,6 +79,9 @@ static inline int down_rows(bool direct, int rank) { return direct && rank <= 12
 template <typename T, bool KC> static int launch_down_form(bool direct, dim3 grid, hipStream_t s, const AdaptersArgs &a)
 {
     if (!direct) return enqueue(adapters_down_any_kernel<T, KC>, grid, dim3(256), s, a);
+    if constexpr (KC) {  // (images of 32 columns that are not K-contiguous have no room for their swizzle)
+        if (a.rank <= 32) return enqueue(adapters_down_kernel<T, 64, 32, 6, KC>, grid, dim3(256), s, a);
+    }
     if (a.rank <= 64) return enqueue(adapters_down_kernel<T, 64, 64, 5, KC>, grid, dim3(256), s, a);
     if (a.rank <= 128) return enqueue(adapters_down_kernel<T, 64, 128, 3, KC>, grid, dim3(256), s, a);
     return enqueue(adapters_down_kernel<T, 32, 256, 4, KC>, grid, dim3(256), s, a);
