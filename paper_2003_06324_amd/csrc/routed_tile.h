@@ -329,10 +329,14 @@ template <typename T, int R, int NT, bool KC> struct GranuleLoader {
         if (__ballot(any) == 0) return;
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {
-            const uint64_t lo = ((uint64_t)v[i][1] << 32) | v[i][0], hi = ((uint64_t)v[i][3] << 32) | v[i][2];
+            // (in words and halves: a 64-bit shift by a number in the wave's last register, v255, has come out wrong here)
             const int s = late[i];
-            const uint64_t l = s == 0 ? lo : (s >= 64 ? hi >> (s - 64) : (lo >> s) | (hi << (64 - s))), h = s >= 64 ? 0 : hi >> s;
-            v[i] = uint4_t{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+            uint4_t w = v[i];
+            w = (s & 64) != 0 ? uint4_t{w[2], w[3], 0u, 0u} : w;
+            w = (s & 32) != 0 ? uint4_t{w[1], w[2], w[3], 0u} : w;
+            if (sizeof(T) == 2)
+                w = (s & 16) != 0 ? uint4_t{(w[0] >> 16) | (w[1] << 16), (w[1] >> 16) | (w[2] << 16), (w[2] >> 16) | (w[3] << 16), w[3] >> 16} : w;
+            v[i] = w;
         }
     }
     __device__ __forceinline__ void store(GEMM_LDS(char) * img, int tid)
