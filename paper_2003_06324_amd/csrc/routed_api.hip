@@ -163,6 +163,14 @@ int wgrad_form(int64_t groups, int64_t M, int64_t N, int64_t num_cu)
     return ceil_div(tiles256 * groups, num_cu) <= 0.6 * (double)ceil_div(tiles128 * groups, 2 * num_cu) ? WGRAD_256x256 : WGRAD_128x128;
 }
 
+// Tile of the product with adapters, likewise (bfloat16, 8 adapters of rank 16 in runs of 140 rows: 5120 rows by 4096 x 2048 152 us on 256 x 256,
+// 118 on 128 x 128, 8192 by 4096 x 4096 266 and 288; where K is short, 8192 by 3584 x 1024, 119 and 110).
+int adapters_form(int64_t rows, int64_t N, int64_t row_bytes, int64_t num_cu)
+{
+    const int64_t tiles256 = ceil_div(rows, 256) * ceil_div(N, 256), tiles128 = ceil_div(rows, 128) * ceil_div(N, 128);
+    return ceil_div(tiles256, num_cu) <= (row_bytes <= 2048 ? 0.48 : 0.6) * (double)ceil_div(tiles128, 2 * num_cu) ? ADAPTERS_256x256 : ADAPTERS_128x128;
+}
+
 template <typename F> int by_kind(int kind, const F &f)
 {
     switch (kind) {
@@ -375,8 +383,9 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         }
         a.A = A, a.B = B, a.down = down, a.lda = lda, a.ldb = ldb, a.ld_down = ld_down, a.stride_down = stride_down;
         const bool fast_now = direct(A, lda, 0, esz) && direct(B, ldb, 0, esz);
-        const int form = fast_now ? (ceil_div(rows, 256) * ceil_div(N, 256) < num_cu ? ADAPTERS_128x128 : ADAPTERS_256x256)
-                                  : (any_large(ceil_div(rows, 128) * ceil_div(N, 128), num_cu) ? ADAPTERS_ANY128 : ADAPTERS_ANY);
+        const int form = fast_now                                                                  ? adapters_form(rows, N, K * esz, num_cu)
+                         : any_large(ceil_div(rows, 128) * ceil_div(N, 128), num_cu) ? ADAPTERS_ANY128
+                                                                                     : ADAPTERS_ANY;
         const int64_t edge = form == ADAPTERS_ANY ? 64 : (form == ADAPTERS_256x256 ? 256 : 128);
         const int64_t tiles_m = ceil_div(rows, edge), tiles_n = ceil_div(N, edge);
         if (tiles_m > (1LL << 24) || tiles_n > (1LL << 24) || tiles_m * tiles_n > (1LL << 24) - 8) return GEMM_ERR_UNSUPPORTED;
