@@ -191,24 +191,38 @@ template <typename T, typename TC> __global__ __launch_bounds__(256) void adapte
     if (a >= 0) {
         const T *const up = (const T *)p.up + (int64_t)a * p.stride_up;
         float4_t add = {0.0f, 0.0f, 0.0f, 0.0f};
-        int q = 0;
-        if (p.up_kc) {
-            for (; q + EPC <= p.rank; q += EPC) {
+        if (p.up_kc && p.rank >= EPC) {
+            auto piece = [&](int at, int from) {  // elements `from` on of the piece at `at`
                 vec_t u[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) u[c] = *(const loose_t *)(up + (int64_t)(col + c < p.N ? col + c : p.N - 1) * p.ld_up + q);
+                for (int c = 0; c < 4; ++c) u[c] = *(const loose_t *)(up + (int64_t)(col + c < p.N ? col + c : p.N - 1) * p.ld_up + at);
 #pragma unroll
-                for (int x = 0; x < EPC; ++x)
+                for (int x = 0; x < EPC; ++x) {
+                    if (x < from) continue;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) add[c] = fmaf(t[q + x], (float)u[c][x], add[c]);
+                    for (int c = 0; c < 4; ++c) add[c] = fmaf(t[at + x], (float)u[c][x], add[c]);
+                }
+            };
+            int q = 0;
+            for (; q + EPC <= p.rank; q += EPC) piece(q, 0);
+            if (q < p.rank) piece(p.rank - EPC, q + EPC - p.rank);
+        } else {
+            constexpr int STEP = 8;
+            const int64_t by_q = p.up_kc ? 1 : p.ld_up, by_col = p.up_kc ? p.ld_up : 1;
+            for (int q0 = 0; q0 < p.rank; q0 += STEP) {
+                T u[STEP][4];
+#pragma unroll
+                for (int x = 0; x < STEP; ++x)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) u[x][c] = up[(q0 + x < p.rank ? q0 + x : p.rank - 1) * by_q + (col + c < p.N ? col + c : p.N - 1) * by_col];
+#pragma unroll
+                for (int x = 0; x < STEP; ++x) {
+                    if (q0 + x >= p.rank) break;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) add[c] = fmaf(t[q0 + x], (float)u[x][c], add[c]);
+                }
             }
         }
-        for (; q < p.rank; ++q)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int j = col + c < p.N ? col + c : p.N - 1;
-                add[c] = fmaf(t[q], (float)up[p.up_kc ? (int64_t)j * p.ld_up + q : (int64_t)q * p.ld_up + j], add[c]);
-            }
         acc += add;
     }
     TC *out = (TC *)p.C + (int64_t)row * p.ldc + col;

@@ -329,12 +329,12 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
         const int64_t num_cu = scratch.num_cu;
         scratch.lock.unlock();
         if (ceil_div(rows, 128) * ceil_div(N, 128) < num_cu / 2 && rows <= 65535) {
-            // few rows: tiles of 64 x 64, K in slices of at least 512 k, one workgroup a CU (64 rows, 4096 x 4096: 4 slices 17.4 us, 2 and 8
+            // few rows: tiles of 64 x 64, K in slices of at least 1 KiB a row, one workgroup a CU (64 rows, 4096 x 4096: 4 slices 17.4 us, 2 and 8
             // 20.4; 256 rows: 2 slices 45, 1 54)
             a.tiles_m = (int)ceil_div(rows, 64);
             a.tiles_n = (int)ceil_div(N, 64);
             const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
-            const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(2, num_cu / tiles), K / 512));
+            const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(2, num_cu / tiles), K * esz / 1024));
             a.k_slice = (int)std::max<int64_t>(64, ceil_div(ceil_div(K, slices), 64) * 64);
             a.slices = (int)ceil_div(K, a.k_slice);
             a.part_pitch = (int)(ceil_div(N, 32) * 32);
@@ -342,8 +342,8 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
                 const int64_t row_tiles = ceil_div(rows, DOWN_ROWS);
                 a.turns = (int)std::min<int64_t>(adapters, DOWN_ROWS);
                 a.t_pitch = (int)(ceil_div(rank, 32) * 32);
-                // slices of at least 256 k, as many as the second launch holds of a row
-                const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(num_cu / row_tiles, JOIN_T / rank), K / 256));
+                // slices of at least 512 bytes a row, as many as the second launch holds of a row
+                const int64_t t_slices = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(num_cu / row_tiles, JOIN_T / rank), K * esz / 512));
                 a.t_k = (int)(ceil_div(ceil_div(K, t_slices), 64) * 64);
                 a.t_slices = (int)ceil_div(K, a.t_k);
                 a.down_groups = (int)ceil_div(row_tiles * a.t_slices * a.turns * a.rank_tiles, DOWN_WAVES);
