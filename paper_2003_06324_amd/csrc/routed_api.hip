@@ -109,18 +109,35 @@ struct Packing {
                        divisor(per_row));
     }
 };
-// Whether the copies pay: through registers a product of 16-bit operands runs at 260 .. 340 TFLOP/s, on direct loads at 550 and more, and
-// what is copied is read and written once, at 4 TB/s or so (32 matrices of 2047 x 2048, 512 rows each: 404 us through registers, 277
-// copied, 148 where only A is; their gradients 262 and 130; adapters, 4096 rows, 2047 x 2048, 138 and 74).  At most half a gigabyte is.
-bool packing_pays(double flops, int64_t bytes) { return bytes > 0 && bytes <= (1LL << 29) && flops > 2e9 + 260.0 * (double)bytes; }
+// Whether the copies pay.  Through registers a product of 16-bit operands runs at 260 TFLOP/s and more, but a tile takes 1.4 us for each of its
+// slabs of 64 k (2 us the weight gradients, of 64 rows); on direct loads at 600, and 0.7 us.  A copy takes 3 us, and
+// what is copied is read and written once, at 4 TB/s or so.  Measured, through registers and copied: 32 matrices of 2047 x 2048, 512 rows each,
+// 404 and 277 us (148 where only A is copied), their gradients 262 and 130; adapters, 4096 rows, 2047 x 2048, 138 and 74; 16 matrices of 1023 x 511,
+// 128 rows each, 20 and 28; the gradients of 7 of 515 x 334, 1500 tokens dealt twice, 19 and 15.  At most half a gigabyte is copied.
+struct PackingWork {
+    double flops;
+    int64_t slabs;   // of a tile
+    double slab_us;  // through registers
+};
+bool packing_pays(const PackingWork &w, int copies, int64_t bytes)
+{
+    if (bytes == 0 || bytes > (1LL << 29)) return false;
+    const double any_us = std::max(w.flops / 260e6, w.slab_us * (double)w.slabs);
+    const double direct_us = std::max(w.flops / 600e6, 0.7 * (double)w.slabs);
+    return direct_us + 3.0 * copies + (double)bytes / 2e6 < any_us;
+}
 
 // Describes the operands that need it as packed, if that pays and there is room for the copies (and for more_bytes, which `more` then
 // points to).  Nothing is enqueued yet: copy() does that.
-template <size_t N> int plan_packing(Packing (&pack)[N], double flops, hipStream_t s, StreamScratch &scratch, int64_t more_bytes = 0, char **more = nullptr)
+template <size_t N> int plan_packing(Packing (&pack)[N], const PackingWork &work, hipStream_t s, StreamScratch &scratch, int64_t more_bytes = 0, char **more = nullptr)
 {
     int64_t bytes = 0;
-    for (const Packing &p : pack) bytes += p.count <= 4096 ? p.bytes() : (1LL << 30);
-    if (!packing_pays(flops, bytes)) bytes = 0;
+    int copies = 0;
+    for (const Packing &p : pack) {
+        bytes += p.count <= 4096 ? p.bytes() : (1LL << 30);
+        copies += p.needed();
+    }
+    if (!packing_pays(work, copies, bytes)) bytes = 0;
     if (bytes + more_bytes == 0) return GEMM_OK;
     int rc = stream_scratch(s, (size_t)(bytes + more_bytes), scratch);
     if (rc != GEMM_OK && bytes > 0) {  // (it works without the copies)
@@ -207,7 +224,7 @@ int gemm_grouped(int kind, int64_t groups, const int32_t *offsets, int64_t rows,
         int64_t none = 0;
         Packing pack[] = {{&A, &lda, &none, 1, a_rows, K}, {&B, &ldb, &strideB, groups, layoutB == GEMM_ROW_MAJOR ? K : N, layoutB == GEMM_ROW_MAJOR ? N : K}};
         if (esz == 2 && K > 0 && a_rows > 0 && (row_map == nullptr || gathers(a_rows, pack[0].pitch(), esz))) {
-            const int rc = plan_packing(pack, 2.0 * (double)rows * (double)N * (double)K, s, scratch);
+            const int rc = plan_packing(pack, {2.0 * (double)rows * (double)N * (double)K, ceil_div(K, 64), 1.4}, s, scratch);
             if (rc != GEMM_OK) return rc;
         }
         int form = GROUPED_ANY;
@@ -256,7 +273,7 @@ int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t
         int64_t none = 0;
         Packing pack[] = {{&A, &lda, &none, 1, a_rows, M}, {&D, &ldd, &none, 1, rows, N}};
         if (esz == 2 && rows >= 64 && a_rows > 0 && (row_map == nullptr ? a_rows >= rows : gathers(a_rows, pack[0].pitch(), esz))) {
-            const int rc = plan_packing(pack, 2.0 * (double)rows * (double)M * (double)N, s, scratch);
+            const int rc = plan_packing(pack, {2.0 * (double)rows * (double)M * (double)N, ceil_div(rows, 64 * groups), 2.0}, s, scratch);
             if (rc != GEMM_OK) return rc;
         }
         // The kernels write rows of C: a column-major C is the row-major C^T = D^T A.
@@ -378,7 +395,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
                           {&down, &ld_down, &stride_down, some ? adapters : 0, dkc ? rank : K, dkc ? K : rank}};
         char *at = nullptr;
         if (esz == 2 || some) {
-            const int rc = plan_packing(pack, esz == 2 ? 2.0 * (double)rows * (double)N * (double)K : 0.0, s, scratch, some ? t_bytes + part_bytes + scale_bytes : 0, &at);
+            const int rc = plan_packing(pack, {esz == 2 ? 2.0 * (double)rows * (double)N * (double)K : 0.0, esz == 2 ? ceil_div(K, 64) : 0, 1.4}, s, scratch, some ? t_bytes + part_bytes + scale_bytes : 0, &at);
             if (rc != GEMM_OK) return rc;
         }
         a.A = A, a.B = B, a.down = down, a.lda = lda, a.ldb = ldb, a.ld_down = ld_down, a.stride_down = stride_down;
