@@ -309,7 +309,8 @@ template <typename T, bool KC> __global__ __launch_bounds__(DOWN_WAVES * 64) voi
 // ---------------------------------------------------------------------------
 // T's slices on direct loads: BM rows and BN columns (rank, rounded up) at once, NST stages of 64 k; every wave multiplies one k-group of a
 // slab, so that a fragment is read from LDS once, and the waves' sums meet in LDS, in wave order.  What bounds it is
-// how much is on its way: 32 rows of the whole K took 58 us at 8192 x 4096 and rank 64, 64 rows in slices of K take 32 .. 37 with runs of 140 rows an adapter, 20 with one adapter.
+// how much is on its way: 32 rows of the whole K took 58 us at 8192 x 4096 and rank 64, 64 rows in slices of K take 32 .. 37 with runs of
+// 140 rows an adapter, 20 with one adapter.
 // ---------------------------------------------------------------------------
 template <typename T, int BM, int BN, int NST, bool KC> __global__ __launch_bounds__(256) void adapters_down_kernel(const AdaptersArgs p)
 {
