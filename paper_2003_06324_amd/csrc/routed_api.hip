@@ -110,20 +110,21 @@ struct Packing {
     }
 };
 // Whether the copies pay.  Through registers a product of 16-bit operands runs at 260 TFLOP/s and more, but a tile takes 1.4 us for each of its
-// slabs of 64 k (2 us the weight gradients, of 64 rows); on direct loads at 600, and 0.7 us.  A copy takes 3 us, and
-// what is copied is read and written once, at 4 TB/s or so.  Measured, through registers and copied: 32 matrices of 2047 x 2048, 512 rows each,
-// 404 and 277 us (148 where only A is copied), their gradients 262 and 130; adapters, 4096 rows, 2047 x 2048, 138 and 74; 16 matrices of 1023 x 511,
-// 128 rows each, 20 and 28; the gradients of 7 of 515 x 334, 1500 tokens dealt twice, 19 and 15.  At most half a gigabyte is copied.
+// slabs of 64 k (the weight gradients, whose tiles are 64 x 64 there: 200 TFLOP/s, 2 us for 64 rows); on direct loads at 600, 0.7 us a slab,
+// 5 us at least.  A copy takes 3 us, and what is copied is read and written once, at 4 TB/s or so.  Measured, through registers and copied:
+// 32 matrices of 2047 x 2048, 512 rows each, 404 and 277 us (148 where only A is copied), their gradients 262 and 130; adapters, 4096 rows,
+// 2047 x 2048, 138 and 74; 16 matrices of 1023 x 511, 128 rows each, 20 and 28; gradients of 7 of 515 x 334, 1500 tokens dealt twice, 19 and
+// 15, of 36 of 627 x 361, 41460 rows, 118 and 72, of 9 of 776 x 1067, 1026 rows, 16 and 24.  At most half a gigabyte is copied.
 struct PackingWork {
     double flops;
     int64_t slabs;   // of a tile
-    double slab_us;  // through registers
+    double slab_us, rate;  // through registers; in flop a microsecond
 };
 bool packing_pays(const PackingWork &w, int copies, int64_t bytes)
 {
     if (bytes == 0 || bytes > (1LL << 29)) return false;
-    const double any_us = std::max(w.flops / 260e6, w.slab_us * (double)w.slabs);
-    const double direct_us = std::max(w.flops / 600e6, 0.7 * (double)w.slabs);
+    const double any_us = std::max(w.flops / w.rate, w.slab_us * (double)w.slabs);
+    const double direct_us = std::max(std::max(w.flops / 600e6, 0.7 * (double)w.slabs), 5.0);
     return direct_us + 3.0 * copies + (double)bytes / 2e6 < any_us;
 }
 
@@ -224,7 +225,7 @@ int gemm_grouped(int kind, int64_t groups, const int32_t *offsets, int64_t rows,
         int64_t none = 0;
         Packing pack[] = {{&A, &lda, &none, 1, a_rows, K}, {&B, &ldb, &strideB, groups, layoutB == GEMM_ROW_MAJOR ? K : N, layoutB == GEMM_ROW_MAJOR ? N : K}};
         if (esz == 2 && K > 0 && a_rows > 0 && (row_map == nullptr || gathers(a_rows, pack[0].pitch(), esz))) {
-            const int rc = plan_packing(pack, {2.0 * (double)rows * (double)N * (double)K, ceil_div(K, 64), 1.4}, s, scratch);
+            const int rc = plan_packing(pack, {2.0 * (double)rows * (double)N * (double)K, ceil_div(K, 64), 1.4, 260e6}, s, scratch);
             if (rc != GEMM_OK) return rc;
         }
         int form = GROUPED_ANY;
@@ -273,7 +274,7 @@ int gemm_grouped_wgrad(int kind, int64_t groups, const int32_t *offsets, int64_t
         int64_t none = 0;
         Packing pack[] = {{&A, &lda, &none, 1, a_rows, M}, {&D, &ldd, &none, 1, rows, N}};
         if (esz == 2 && rows >= 64 && a_rows > 0 && (row_map == nullptr ? a_rows >= rows : gathers(a_rows, pack[0].pitch(), esz))) {
-            const int rc = plan_packing(pack, {2.0 * (double)rows * (double)M * (double)N, ceil_div(rows, 64 * groups), 2.0}, s, scratch);
+            const int rc = plan_packing(pack, {2.0 * (double)rows * (double)M * (double)N, ceil_div(rows, 64 * groups), 2.0, 200e6}, s, scratch);
             if (rc != GEMM_OK) return rc;
         }
         // The kernels write rows of C: a column-major C is the row-major C^T = D^T A.
@@ -395,7 +396,7 @@ int gemm_adapters(int kind, int64_t rows, int64_t N, int64_t K, const void *A, i
                           {&down, &ld_down, &stride_down, some ? adapters : 0, dkc ? rank : K, dkc ? K : rank}};
         char *at = nullptr;
         if (esz == 2 || some) {
-            const int rc = plan_packing(pack, {esz == 2 ? 2.0 * (double)rows * (double)N * (double)K : 0.0, esz == 2 ? ceil_div(K, 64) : 0, 1.4}, s, scratch, some ? t_bytes + part_bytes + scale_bytes : 0, &at);
+            const int rc = plan_packing(pack, {esz == 2 ? 2.0 * (double)rows * (double)N * (double)K : 0.0, esz == 2 ? ceil_div(K, 64) : 0, 1.4, 260e6}, s, scratch, some ? t_bytes + part_bytes + scale_bytes : 0, &at);
             if (rc != GEMM_OK) return rc;
         }
         a.A = A, a.B = B, a.down = down, a.lda = lda, a.ldb = ldb, a.ld_down = ld_down, a.stride_down = stride_down;
